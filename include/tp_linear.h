@@ -308,6 +308,45 @@ int tp_bias_grad(const void* da, int64_t ld_da, int64_t rows, int64_t cols, void
 /* Bytes of workspace the slab form of tp_bias_grad wants (0: it would not split the rows).  Host only. */
 size_t tp_bias_grad_workspace_size(int64_t rows, int64_t cols);
 
+/*
+ * Dropout beside the layer, with a mask that is never stored.  Element (R, C) of the FULL matrix (R, C: its row and column there) is kept
+ * where its 16 random bits are at least T = p 65536 rounded to the nearest integer, and then multiplied by 65536 / (65536 - T); a dropped one is 0,
+ * whatever it was, NaN included.  The bits are Philox4x32-10 of the counter {C / 8, R, offset low, offset high} under the key {seed low, seed
+ * high} (Salmon, Moraes, Dror, Shaw 2011): columns 8 g .. 8 g + 7 share one draw of four words, column 8 g + 2 i its word i's low half,
+ * column 8 g + 2 i + 1 the high half.  So every rank of every grid draws its own part of one and the same mask, and backward draws it again.
+ *   seed, offset : which mask: a number of its own for every layer and step.
+ *   offset_dev   : optional DEVICE uint64, 8-byte aligned: added to offset (mod 2^64) when the kernels run, so that replays of a captured graph
+ *                  draw new masks.
+ *   row0, col0   : where the block's first element lies in the full matrix; col0 a multiple of 8.
+ *   p            : probability of dropping, 0 <= p <= 1 (p = 1 drops everything).
+ * Refused: p outside [0, 1] or NaN (TP_ERR_MODE), col0 not a multiple of 8 or offset_dev misaligned (TP_ERR_ALIGN), negative positions, rows that
+ * end beyond 2^32 or columns beyond 2^35 (TP_ERR_SHAPE).
+ */
+typedef struct { uint64_t seed, offset; const uint64_t* offset_dev; int64_t row0, col0; double p; } tp_dropout_t;
+
+/*
+ * tp_dropout_fwd -- what follows a product or the summation of its partials, with dropout:
+ *     A = x + bias,   y = drop(GeLU(A)) + residual  (epi TP_EPI_BIAS_GELU; TP_EPI_BIAS: drop(A) + residual; TP_EPI_NONE: drop(x) + residual)
+ *   x        : fp32 or bf16 (x_dtype) [rows, cols];  bias: bf16 [cols] or NULL with TP_EPI_NONE;
+ *   residual : optional bf16 [rows, cols] (NULL ptr: none);  y: fp32 or bf16;  preact: optional bf16 copy of A.
+ * y may be x or residual itself (same address, type and leading dimension).  cols and every ld multiples of 8.  HBM-bound.
+ * Defined by: Section 2.2, 1D paragraph and the chunk shapes of 2D / 2.5D / 3D, as tp_bias_act: what is applied to a rank's chunk of the output
+ * once it exists.  Nothing is done with rows = 0 or cols = 0 (blocks may be NULL then).
+ * Errors: TP_ERR_NULL, TP_ERR_MODE, TP_ERR_SHAPE, TP_ERR_ALIGN, TP_ERR_DTYPE, TP_ERR_HIP.
+ */
+int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_dtype, const void* bias, int epi, tp_cblk_t residual,
+                   tp_oblk_t y, tp_oblk_t preact, int64_t rows, int64_t cols, void* hip_stream);
+
+/*
+ * tp_dropout_bwd -- its gradient:  dx = drop'(dy) GeLU'(preact)  (without preact: drop'(dy)), bf16, and optionally db (fp32 [cols]): the
+ * column sums of dx before its rounding, in an order fixed by (rows, cols) and whether there is a workspace.  The residual's gradient is dy itself.
+ *   drop      : as in forward.   dy, preact, dx: bf16 [rows, cols];  dx may be dy itself.
+ *   workspace : as in tp_bias_grad (tp_bias_grad_workspace_size(rows, cols) bytes, 16-byte aligned, or NULL); read only if db is wanted.
+ * With rows = 0 db is all zeros (blocks may be NULL then).  Errors: as tp_dropout_fwd, and TP_ERR_WORKSPACE.
+ */
+int tp_dropout_bwd(const tp_dropout_t* drop, const void* dy, int64_t ld_dy, const void* preact, int64_t ld_pre, void* dx, int64_t ld_dx,
+                   void* db_f32, int64_t rows, int64_t cols, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Human-readable name of a status code (static storage). */
 const char* tp_strerror(int status);
 

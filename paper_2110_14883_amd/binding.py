@@ -13,6 +13,7 @@ import importlib.util
 import os
 import sys
 from dataclasses import dataclass
+from typing import Any, NamedTuple
 
 MODE_1D_COL, MODE_1D_ROW, MODE_2D, MODE_2P5D, MODE_3D, MODE_3D_GATHERED = 10, 11, 2, 25, 3, 33
 EPI_NONE, EPI_BIAS, EPI_BIAS_GELU = 0, 1, 2
@@ -46,6 +47,21 @@ class _CBlk(C.Structure):
 
 class _OBlk(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("ld", C.c_int64), ("dtype", C.c_int)]
+
+
+class _DropoutS(C.Structure):
+    _fields_ = [("seed", C.c_uint64), ("offset", C.c_uint64), ("offset_dev", C.c_void_p), ("row0", C.c_int64), ("col0", C.c_int64), ("p", C.c_double)]
+
+
+class Dropout(NamedTuple):
+    """A dropout mask (tp_dropout_t): probability, which mask (seed, offset and optionally a device uint64 / int64 tensor of one element
+    that is added to offset when the kernels run), and where the block begins in the full matrix."""
+    p: float
+    seed: int
+    offset: int = 0
+    offset_dev: Any = None
+    row0: int = 0
+    col0: int = 0
 
 
 class _PlanOpts(C.Structure):
@@ -149,6 +165,12 @@ def lib() -> C.CDLL:
         L.tp_bias_grad.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.tp_bias_grad_workspace_size.restype = C.c_size_t
         L.tp_bias_grad_workspace_size.argtypes = [C.c_int64, C.c_int64]
+        dp = C.POINTER(_DropoutS)
+        L.tp_dropout_fwd.restype = C.c_int
+        L.tp_dropout_fwd.argtypes = [dp, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int, _CBlk, _OBlk, _OBlk, C.c_int64, C.c_int64, C.c_void_p]
+        L.tp_dropout_bwd.restype = C.c_int
+        L.tp_dropout_bwd.argtypes = [dp, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
+                                     C.c_void_p, C.c_size_t, C.c_void_p]
         L.tp_strerror.restype = C.c_char_p
         L.tp_strerror.argtypes = [C.c_int]
         _lib = L
@@ -166,19 +188,20 @@ def _call():
     spec.loader.exec_module(m)
     try:
         import torch
-        dtypes = (torch.float32, torch.bfloat16)
+        dtypes, device = (torch.float32, torch.bfloat16), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     except ImportError:                      # blocks are then (address, leading dimension[, dtype]) sequences
-        dtypes = (None, None)
+        dtypes, device = (None, None), None
     names = ("tp_linear_fwd_ex", "tp_linear_fwd_static", "tp_linear_bwd_ex", "tp_linear_bwd_partials_ex", "tp_bias_act", "tp_dgelu",
              "tp_bias_grad")
     m.bind(*[C.cast(getattr(L, n), C.c_void_p).value for n in names], *dtypes)
+    m.bind_ops(*[C.cast(getattr(L, n), C.c_void_p).value for n in ("tp_dropout_fwd", "tp_dropout_bwd")], device)
     return m
 
 
 EXPORTS = ("tp_block_map", "tp_linear_workspace_size", "tp_linear_workspace_size_ex", "tp_linear_fwd", "tp_linear_fwd_ex",
            "tp_linear_bwd", "tp_linear_bwd_ex", "tp_dgelu", "tp_partials_map", "tp_linear_bwd_partials",
            "tp_linear_bwd_partials_ex", "tp_bias_act", "tp_bias_grad", "tp_strerror", "tp_linear_fwd_static",
-           "tp_static_scratch_bytes", "tp_bias_grad_workspace_size")
+           "tp_static_scratch_bytes", "tp_bias_grad_workspace_size", "tp_dropout_fwd", "tp_dropout_bwd")
 
 
 # ----------------------------------------------------------------------------- marshalling helpers
@@ -309,3 +332,17 @@ def tp_bias_grad(da, db, rows: int | None = None, cols: int | None = None, works
 
 def tp_bias_grad_workspace_size(rows: int, cols: int) -> int:
     return int(lib().tp_bias_grad_workspace_size(int(rows), int(cols)))
+
+
+def tp_dropout_fwd(dropout: Dropout, x, bias, epi: int, y, residual=None, preact=None, rows: int | None = None, cols: int | None = None,
+                   stream=None) -> None:
+    """y = drop(act(x + bias)) + residual; x: fp32 or bf16."""
+    rows, cols = _rows_cols(x, rows, cols)
+    _check(_call().dropout_fwd(dropout, x, bias, epi, residual, y, preact, rows, cols, _stream(stream)), "tp_dropout_fwd")
+
+
+def tp_dropout_bwd(dropout: Dropout, dy, dx, preact=None, db=None, rows: int | None = None, cols: int | None = None, workspace=None,
+                   stream=None) -> None:
+    """dx = drop'(dy) GeLU'(preact); db: its column sums (workspace: as tp_bias_grad)."""
+    rows, cols = _rows_cols(dy, rows, cols)
+    _check(_call().dropout_bwd(dropout, dy, preact, dx, db, rows, cols, workspace, _stream(stream)), "tp_dropout_bwd")

@@ -7,6 +7,7 @@
 #include <cstdint>
 #include <cstring>
 
+#include "tp_checks.h"
 #include "tp_internal.h"
 
 using namespace tpl;
@@ -14,7 +15,6 @@ using namespace tpl;
 namespace {
 
 constexpr int kCUs = 256;                       // MI355X compute units (8 XCDs x 32): the tile order and the plan assume it
-constexpr int64_t kMaxLd = (int64_t)1 << 21;    // keeps every in-tile byte offset below 2^31
 
 // Launch-plan options of one call, resolved from the caller's tp_plan_opts_t (NULL = automatic).
 // rotate: -1 automatic (on for the eight-wave kernel, off for the four-wave stream kernel: its workgroups
@@ -356,23 +356,6 @@ Plan make_plan(const Opts& o, int form, int64_t m, int64_t n, int64_t k, int n_s
     return p;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int check_cblk(const tp_cblk_t& b, int64_t cols) {
-    if (!b.ptr) return TP_ERR_NULL;
-    if (!aligned16(b.ptr) || (b.ld & 7) || (cols & 7)) return TP_ERR_ALIGN;
-    if (b.ld < cols || b.ld > kMaxLd) return TP_ERR_SHAPE;
-    return TP_OK;
-}
-int check_oblk(const tp_oblk_t& b, int64_t cols, bool f32_only) {
-    if (!b.ptr) return TP_ERR_NULL;
-    if (b.dtype != TP_BF16 && b.dtype != TP_F32) return TP_ERR_DTYPE;
-    if (f32_only && b.dtype != TP_F32) return TP_ERR_DTYPE;
-    if (!aligned16(b.ptr) || (b.ld & 7) || (cols & 7)) return TP_ERR_ALIGN;
-    if (b.ld < cols) return TP_ERR_SHAPE;
-    return TP_OK;
-}
-
 struct Product {                 // one validated GEMM ready to launch
     int form; Plan plan; GemmArgs args; bool active;
     bool four_wave;              // on the four-wave (and workgroup-split) kernels; else on the eight-wave one
@@ -453,14 +436,6 @@ int run_product(const Opts& o, const Product& pr, void* workspace, hipStream_t s
     return run_one(o, pr.form, pr.four_wave, pl.tail_tile_id, pl.tail_split, tail, stream);
 }
 
-// Bytes a product reads or writes: the span of one block of rows x cols (es bytes an element)
-struct Range { uintptr_t lo, hi; };
-Range span(const void* p, int64_t ld, int64_t rows, int64_t cols, int es) {
-    const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-    return Range{lo, lo + (uintptr_t)(((rows - 1) * ld + cols) * es)};
-}
-bool overlap(const Range& a, const Range& b) { return a.lo < b.hi && b.lo < a.hi; }
-
 // whether `w` writes anything that `r` reads or writes
 bool writes_into(const GemmArgs& w, int form, const GemmArgs& r) {
     const int outs = w.n_groups > 1 ? w.n_groups : 1, slots = r.n_groups > 1 ? r.n_groups : r.n_steps, r_outs = r.n_groups > 1 ? r.n_groups : 1;
@@ -508,10 +483,6 @@ void plan_product(const Opts& o, Product& pr) {
         a.group_tiles = a.group_along_n ? p.tiles_n : p.tiles_m;
         (a.group_along_n ? a.tiles_n : a.tiles_m) *= groups;
     }
-}
-
-bool ws_ok(size_t need, const void* workspace, size_t bytes) {
-    return need == 0 || (workspace && bytes >= need && aligned16(workspace));
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -37,6 +37,21 @@ inline hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, siz
     return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, ptrs, lds_bytes, stream);
 }
 
+// f(first row, rows, threads, Divisor): launches over the rows of a block, at most 2^31 - 1 threads each
+template <class F>
+inline hipError_t over_rows(int64_t rows, int64_t per_row, F&& f) {
+    if (rows <= 0 || per_row <= 0) return hipSuccess;
+    if (per_row >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+    const Divisor d = divisor((uint32_t)per_row);
+    const int64_t most = (((int64_t)1 << 31) - 1) / per_row;
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = rows - r < most ? rows - r : most;
+        if (hipError_t e = f(r, n, (uint32_t)(n * per_row), d); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+inline dim3 covering(uint32_t threads) { return dim3((threads + 255u) / 256u); }
+
 // ---------------------------------------------------------------------------------------------
 // small device helpers
 // ---------------------------------------------------------------------------------------------

@@ -66,6 +66,20 @@ struct ReduceArgs {
     const void* dg; int64_t lddg;
 };
 
+// A dropout mask (tp_dropout_t) as the kernels take it: position of the block's first row and first group of eight columns
+struct DropArgs {
+    uint32_t key0, key1;
+    uint64_t offset;
+    const uint64_t* offset_dev;          // added to the offset by the kernel, or null
+    uint32_t threshold;                  // 0 .. 65536: columns whose 16 bits are below it are dropped
+    float factor;                        // of those that are kept
+    uint32_t row0, group0;
+};
+hipError_t launch_dropout(const DropArgs& drop, const void* x, int64_t ldx, int x_f32, const void* bias, int gelu, const void* res, int64_t ldr, void* y,
+                          int64_t ldy, int y_f32, void* pre, int64_t ldp, int64_t rows, int64_t cols, hipStream_t stream);
+hipError_t launch_dropout_bwd(const DropArgs& drop, const void* dy, int64_t ld_dy, const void* pre, int64_t ld_pre, void* dx, int64_t ld_dx, int64_t rows,
+                              int64_t cols, float* db, float* ws, hipStream_t stream);     // db (ws: colsum_ws_bytes or null) may be null
+
 // tile ids: macro-tile shapes the GEMM kernel is instantiated for
 enum TileId { TILE_256x256 = 1, TILE_128x256 = 2, TILE_256x128 = 3, TILE_128x128 = 4,
               TILE_256x256_W4 = 5,     // 256 x 256 by the four-wave stream kernel (tp_gemm4.hip)
@@ -87,6 +101,9 @@ hipError_t launch_colsum(const void* da, int64_t ld, int64_t rows, int64_t cols,
 hipError_t launch_dgelu_colsum(const void* dy, int64_t ld_dy, const void* pre, int64_t ld_pre, void* da, int64_t ld, int64_t rows,
                                int64_t cols, float* out, float* ws, hipStream_t stream);     // both in one pass where that pays
 size_t colsum_ws_bytes(int64_t rows, int64_t cols);     // 0: the column sum needs no workspace
+struct ColsumPlan { int splits; bool wide; int64_t per; };   // how a column sum runs: slabs of rows, strips of 128 columns or 64, rows of a slab
+ColsumPlan colsum_plan(int64_t rows, int64_t cols, bool has_ws, bool from_dy);
+hipError_t launch_colsum_finish(const float* ws, int splits, int64_t cols, float* out, hipStream_t stream);    // out = the slabs' sums added up
 // y = [GeLU](c + bias) over an fp32 [rows][cols] block, optional bf16 copy of c + bias
 hipError_t launch_bias_act(const float* c, int64_t ldc, const void* bias, int gelu, void* y, int64_t ldy, int y_f32,
                            void* pre, int64_t ldp, int64_t rows, int64_t cols, hipStream_t stream);

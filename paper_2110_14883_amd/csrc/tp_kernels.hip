@@ -592,21 +592,6 @@ hipError_t launch_gemm(int form, int tile_id, const GemmArgs& args, hipStream_t 
     }
 }
 
-// f(first row, rows, threads, Divisor): launches over the rows of a block, at most 2^31 - 1 threads each
-template <class F>
-static hipError_t over_rows(int64_t rows, int64_t per_row, F&& f) {
-    if (rows <= 0 || per_row <= 0) return hipSuccess;
-    if (per_row >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-    const Divisor d = divisor((uint32_t)per_row);
-    const int64_t most = (((int64_t)1 << 31) - 1) / per_row;
-    for (int64_t r = 0; r < rows; r += most) {
-        const int64_t n = rows - r < most ? rows - r : most;
-        if (hipError_t e = f(r, n, (uint32_t)(n * per_row), d); e != hipSuccess) return e;
-    }
-    return hipSuccess;
-}
-static dim3 covering(uint32_t threads) { return dim3((threads + 255u) / 256u); }
-
 template <int Z>
 static hipError_t reduce_planes(const ReduceArgs& a, hipStream_t s) {
     return over_rows(a.M, a.N >> 2, [&](int64_t r, int64_t n, uint32_t total, Divisor d) {
@@ -676,8 +661,7 @@ size_t colsum_ws_bytes(int64_t rows, int64_t cols) {
     const int r = colsum_splits(rows, cols);
     return r > 1 ? (size_t)r * (size_t)cols * 4 : 0;
 }
-// How the sum runs.  Times in us, replayed graphs.
-struct ColsumPlan { int splits; bool wide; int64_t per; };
+// Times in us, replayed graphs.
 ColsumPlan colsum_plan(int64_t rows, int64_t cols, bool has_ws, bool from_dy) {
     ColsumPlan p;
     // up to 512 rows one slab: a second one costs the finish launch (300 x 1024: 3.1 against 4.8, 300 x 8192 3.3 / 5.0)
@@ -692,6 +676,9 @@ ColsumPlan colsum_plan(int64_t rows, int64_t cols, bool has_ws, bool from_dy) {
     p.wide = strips * p.splits > 128 && (rows >= 1024 || (from_dy && (p.splits == 1 || strips * p.splits > 256)));
     return p;
 }
+hipError_t launch_colsum_finish(const float* ws, int splits, int64_t cols, float* out, hipStream_t s) {
+    return launch_kernel(tp_colsum_finish_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(256), 0, s, ws, splits, (int)cols, out);
+}
 template <bool FROM_DY, int COLS>
 static hipError_t colsum_passes(const ColsumPlan& p, const uint16_t* dy, int64_t ld_dy, const uint16_t* pre, int64_t ld_pre, uint16_t* da,
                                 int64_t ld, int64_t rows, int64_t cols, float* out, float* ws, hipStream_t s) {
@@ -699,8 +686,7 @@ static hipError_t colsum_passes(const ColsumPlan& p, const uint16_t* dy, int64_t
     if (hipError_t e = launch_kernel(tp_colsum_kernel<FROM_DY, COLS>, dim3(strips, (unsigned)p.splits), dim3(COLS * 4), 0, s, dy, ld_dy,
                                      pre, ld_pre, da, ld, rows, (int)cols, p.splits == 1 ? out : ws, p.per); e != hipSuccess || p.splits == 1)
         return e;
-    return launch_kernel(tp_colsum_finish_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(256), 0, s,
-                         static_cast<const float*>(ws), p.splits, (int)cols, out);
+    return launch_colsum_finish(ws, p.splits, cols, out, s);
 }
 // ws: colsum_ws_bytes(rows, cols) bytes, or null for the single-slab form
 hipError_t launch_colsum(const void* da, int64_t ld, int64_t rows, int64_t cols, float* out, float* ws, hipStream_t s) {

@@ -17,7 +17,9 @@
 namespace {
 
 PyObject *s_data_ptr, *s_stride, *s_shape, *s_dtype, *s_numel, *s_element_size;      // interned names
+PyObject *s_get_device;
 PyObject *g_f32, *g_bf16;                                                            // torch.float32, torch.bfloat16
+PyObject *g_current_device;                                                          // callable, or None: its answer is not compared
 
 decltype(&tp_linear_fwd_ex) f_fwd;
 decltype(&tp_linear_fwd_static) f_static;
@@ -26,6 +28,8 @@ decltype(&tp_linear_bwd_partials_ex) f_partials;
 decltype(&tp_bias_act) f_bias_act;
 decltype(&tp_dgelu) f_dgelu;
 decltype(&tp_bias_grad) f_bias_grad;
+decltype(&tp_dropout_fwd) f_dropout_fwd;
+decltype(&tp_dropout_bwd) f_dropout_bwd;
 
 // Every helper returns false with a Python exception set.
 struct Ref {                                       // an owned reference
@@ -287,7 +291,83 @@ PyObject* bias_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return nullptr;
     return answer([&] { return f_bias_grad(da.ptr, da.ld, rows, cols, db, ws.ptr, ws.bytes, stream); });
 }
-// bind(addresses of the seven functions in the order above, torch.float32, torch.bfloat16)
+// The calls below also look at what the C functions cannot see of a tensor: its type, where only one fits, and that all of a call's
+// tensors are on the current device (a kernel that follows a host address ends the process).
+struct Devices {
+    int64_t seen = -1;
+    bool add(PyObject* t) {
+        int64_t d;
+        if (!call0(t, s_get_device, &d)) return false;
+        if (d < 0) { PyErr_SetString(PyExc_ValueError, "a tensor of the call is not on the GPU"); return false; }
+        if (seen >= 0) {
+            if (d == seen) return true;
+        } else {
+            seen = d;
+            if (!g_current_device || g_current_device == Py_None) return true;
+            Ref r(PyObject_CallNoArgs(g_current_device));
+            int64_t now;
+            if (!r || !to_i64(r.p, &now)) return false;
+            if (d == now) return true;
+        }
+        PyErr_SetString(PyExc_ValueError, "the call's tensors are not all on the current device");
+        return false;
+    }
+};
+// None, an address or sequence (taken as it is), or a tensor on the current device, of type `want` if that is given
+bool look(PyObject* o, PyObject* want, Devices* at) {
+    if (o == Py_None || PyLong_Check(o)) return true;
+    bool tensor;
+    if (!is_tensor(o, &tensor)) return false;
+    if (!tensor) return true;
+    if (!at->add(o)) return false;
+    if (!want || want == Py_None) return true;
+    Ref dt(PyObject_GetAttr(o, s_dtype));
+    if (!dt) return false;
+    if (dt.p == want) return true;
+    PyErr_Format(PyExc_TypeError, "%R expected, got %R", want, dt.p);
+    return false;
+}
+
+// A mask: a sequence (p, seed, offset, offset_dev, row0, col0)
+bool to_dropout(PyObject* o, tp_dropout_t* d, Devices* at) {
+    Ref s(PySequence_Fast(o, "dropout must be a Dropout"));
+    if (!s) return false;
+    if (PySequence_Fast_GET_SIZE(s.p) != 6) {
+        PyErr_SetString(PyExc_ValueError, "dropout must be a Dropout: (p, seed, offset, offset_dev, row0, col0)");
+        return false;
+    }
+    PyObject** it = PySequence_Fast_ITEMS(s.p);
+    d->p = PyFloat_AsDouble(it[0]);
+    if (d->p == -1.0 && PyErr_Occurred()) return false;
+    int64_t seed, offset;
+    void* dev;
+    if (!to_i64(it[1], &seed) || !to_i64(it[2], &offset) || !look(it[3], nullptr, at) || !to_ptr(it[3], &dev) || !to_i64(it[4], &d->row0) || !to_i64(it[5], &d->col0)) return false;
+    d->seed = (uint64_t)seed;
+    d->offset = (uint64_t)offset;
+    d->offset_dev = static_cast<const uint64_t*>(dev);
+    return true;
+}
+// dropout_fwd(dropout, x, bias, epi, residual, y, preact, rows, cols, stream)
+PyObject* dropout_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    tp_dropout_t d; tp_oblk_t x, y, pre; tp_cblk_t res; void *bias, *stream; int epi; int64_t rows, cols; Devices at;
+    if (!count(n, 10) || !look(a[1], nullptr, &at) || !look(a[2], g_bf16, &at) || !look(a[4], g_bf16, &at) || !look(a[5], nullptr, &at) ||
+        !look(a[6], nullptr, &at) || !to_dropout(a[0], &d, &at) || !to_oblk(a[1], &x) || !to_ptr(a[2], &bias) || !to_int(a[3], &epi) || !to_cblk(a[4], &res) ||
+        !to_oblk(a[5], &y) || !to_oblk(a[6], &pre) || !to_i64(a[7], &rows) || !to_i64(a[8], &cols) || !to_ptr(a[9], &stream))
+        return nullptr;
+    return answer([&] { return f_dropout_fwd(&d, x.ptr, x.ld, x.dtype, bias, epi, res, y, pre, rows, cols, stream); });
+}
+// dropout_bwd(dropout, dy, preact, dx, db, rows, cols, workspace, stream)
+PyObject* dropout_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    tp_dropout_t d; tp_cblk_t dy, pre, dx; void *db, *stream; int64_t rows, cols; Workspace ws; Devices at;
+    if (!count(n, 9) || !look(a[1], g_bf16, &at) || !look(a[2], g_bf16, &at) || !look(a[3], g_bf16, &at) || !look(a[4], g_f32, &at) ||
+        !look(a[7], nullptr, &at) || !to_dropout(a[0], &d, &at) || !to_cblk(a[1], &dy) || !to_cblk(a[2], &pre) || !to_cblk(a[3], &dx) || !to_ptr(a[4], &db) ||
+        !to_i64(a[5], &rows) || !to_i64(a[6], &cols) || !to_ws(a[7], &ws) || !to_ptr(a[8], &stream))
+        return nullptr;
+    return answer([&] {
+        return f_dropout_bwd(&d, dy.ptr, dy.ld, pre.ptr, pre.ld, const_cast<void*>(dx.ptr), dx.ld, db, rows, cols, ws.ptr, ws.bytes, stream);
+    });
+}
+// bind(addresses of the first seven functions in the order above, torch.float32, torch.bfloat16)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* f[7];
     if (!count(n, 9)) return nullptr;
@@ -305,15 +385,29 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+// bind_ops(addresses of the functions behind those, a function that gives the current device or None)
+PyObject* bind_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void* f[2];
+    if (!count(n, 3)) return nullptr;
+    for (int i = 0; i < 2; ++i)
+        if (!to_ptr(a[i], &f[i])) return nullptr;
+    Py_INCREF(a[2]); Py_XSETREF(g_current_device, a[2]);
+    f_dropout_fwd = reinterpret_cast<decltype(f_dropout_fwd)>(f[0]);
+    f_dropout_bwd = reinterpret_cast<decltype(f_dropout_bwd)>(f[1]);
+    Py_RETURN_NONE;
+}
+
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
 PyMethodDef methods[] = {{"fwd", FAST(fwd)}, {"fwd_static", FAST(fwd_static)}, {"bwd", FAST(bwd)}, {"bwd_partials", FAST(bwd_partials)},
                          {"bias_act", FAST(bias_act)}, {"dgelu", FAST(dgelu)}, {"bias_grad", FAST(bias_grad)}, {"bind", FAST(bind)},
+                         {"dropout_fwd", FAST(dropout_fwd)}, {"dropout_bwd", FAST(dropout_bwd)}, {"bind_ops", FAST(bind_ops)},
                          {nullptr, nullptr, 0, nullptr}};
 // (Set up in its exec slot: a second load of the file makes a module of its own.  A module set up in one go would fill the one that stands under
 // this name in sys.modules, which may be another copy's.)
 int exec(PyObject*) {
     struct { PyObject** to; const char* name; } names[] = {{&s_data_ptr, "data_ptr"}, {&s_stride, "stride"}, {&s_shape, "shape"},
-                                                           {&s_dtype, "dtype"}, {&s_numel, "numel"}, {&s_element_size, "element_size"}};
+                                                           {&s_dtype, "dtype"}, {&s_numel, "numel"}, {&s_element_size, "element_size"},
+                                                           {&s_get_device, "get_device"}};
     for (auto& x : names)
         if (!*x.to && !(*x.to = PyUnicode_InternFromString(x.name))) return -1;
     return 0;

@@ -1,0 +1,302 @@
+"""Dropout without a stored mask: the generator against its published test vectors and against a plain implementation, forward and
+backward against 64 bits, what the calls refuse, and the mask under partitions, captured graphs and other streams."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2110_14883_amd as T
+from paper_2110_14883_amd import binding as B
+
+W = 0xFFFFFFFF
+
+
+def philox(counter, key):
+    """Philox4x32-10 of four 32-bit counter words (arrays) under two key words, as published; numpy in 64 bits."""
+    x = [np.asarray(c, dtype=np.uint64) for c in counter]
+    k = [int(key[0]), int(key[1])]
+    for _ in range(10):
+        a, b = x[0] * np.uint64(0xD2511F53), x[2] * np.uint64(0xCD9E8D57)
+        s, m = np.uint64(32), np.uint64(W)
+        x = [(b >> s) ^ x[1] ^ np.uint64(k[0]), b & m, (a >> s) ^ x[3] ^ np.uint64(k[1]), a & m]
+        k = [(k[0] + 0x9E3779B9) & W, (k[1] + 0xBB67AE85) & W]
+    return x
+
+
+def keep_mask(d, rows, cols):
+    """Truth values [rows, cols] of the mask's definition; d: (p, seed, offset, row0, col0)."""
+    p, seed, offset, row0, col0 = d
+    r = (np.arange(rows, dtype=np.uint64) + np.uint64(row0))[:, None]
+    g = (np.arange(cols // 8, dtype=np.uint64) + np.uint64(col0 // 8))[None]
+    r, g = np.broadcast_arrays(r, g)
+    offset %= 1 << 64
+    words = philox((g, r, np.full_like(g, offset & W), np.full_like(g, offset >> 32)), (seed & W, (seed >> 32) & W))
+    bits = np.stack([h for w in words for h in (w & np.uint64(0xFFFF), w >> np.uint64(16))], axis=2).reshape(rows, cols)
+    return bits >= round(p * 65536)
+
+
+def factor(p):
+    t = round(p * 65536)
+    return 65536.0 / (65536 - t) if t < 65536 else 0.0
+
+
+def gelu64(a):
+    return a * 0.5 * torch.special.erfc(-a * math.sqrt(0.5))
+
+
+def slope64(a):
+    return 0.5 * torch.special.erfc(-a * math.sqrt(0.5)) + a * torch.exp(-a * a / 2) / math.sqrt(2 * math.pi)
+
+
+def near(got, ref, dtype, work=0.0):
+    """got within half a step of its type of ref, plus `work` (absolute: what 32-bit arithmetic may have lost before that rounding)."""
+    got, ref = got.double().cpu(), ref.double().cpu()
+    tol = ref.abs() * (torch.finfo(dtype).eps / 2) * 1.001 + work
+    bad = ~((got - ref).abs() <= tol)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} elements off, worst {((got - ref).abs() - tol).max()}"
+
+
+def test_generator_published_vectors():
+    """The known answers that the authors publish with the generator."""
+    for counter, key, want in (((0, 0, 0, 0), (0, 0), (0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8)),
+                               ((W, W, W, W), (W, W), (0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD)),
+                               ((0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344), (0xA4093822, 0x299F31D0), (0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1))):
+        assert tuple(int(w) for w in philox(counter, key)) == want
+
+
+def test_plain_mask_keeps_the_share_it_says():
+    """16 bits a column: over 2^20 columns the kept share is within five standard deviations, for every column of a group."""
+    for p in (0.0, 0.1, 0.5, 0.9):
+        k = keep_mask((p, 99, 3, 0, 0), 1024, 1024)
+        sd = math.sqrt(max(p * (1 - p), 1e-9) / (k.size / 8))
+        for e in range(8):
+            assert abs(k[:, e::8].mean() - (1 - p)) <= 5 * sd + 1 / 65536
+    assert not keep_mask((1.0, 1, 0, 0, 0), 8, 64).any()
+
+
+def _st(fn):
+    try:
+        fn()
+    except T.TpError as e:
+        return e.status
+    return 0
+
+
+def test_refusals():
+    """Found on the host: the addresses are never followed."""
+    D, x, y = T.Dropout, (0x10000, 64, B.DT_F32), (0x20000, 64, B.DT_BF16)
+    fwd = lambda **k: _st(lambda: T.tp_dropout_fwd(k.get("d", D(0.1, 1)), k.get("x", x), k.get("bias", 0x30000), k.get("epi", T.EPI_BIAS), k.get("y", y),
+                                                   k.get("res"), k.get("pre"), k.get("rows", 4), k.get("cols", 64), stream=0))
+    for p in (-0.1, 1.0001, float("nan"), float("inf")):
+        assert fwd(d=D(p, 1)) == 2
+    assert fwd(d=D(0.1, 1, col0=4)) == 5 and fwd(d=D(0.1, 1, offset_dev=0x1004)) == 5
+    assert fwd(d=D(0.1, 1, row0=-1)) == 4 and fwd(d=D(0.1, 1, col0=-8)) == 4
+    assert fwd(d=D(0.1, 1, row0=2 ** 32 - 3)) == 4 and fwd(d=D(0.1, 1, col0=2 ** 35 - 56)) == 4 and fwd(d=D(0.1, 1, row0=2 ** 62)) == 4
+    assert fwd(x=(0, 64, 1)) == 1 and fwd(y=(0, 64, 1)) == 1 and fwd(bias=None) == 1 and fwd(epi=7) == 2
+    assert fwd(x=(0x10000, 64, 5)) == 6 and fwd(y=(0x20000, 64, 5)) == 6 and fwd(pre=(0x50000, 64, B.DT_F32)) == 6
+    assert fwd(x=(0x10008, 64, 1)) == 5 and fwd(x=(0x10000, 60, 1)) == 5 and fwd(x=(0x10000, 56, 1)) == 4 and fwd(bias=0x30008) == 5
+    assert fwd(res=(0x40008, 64)) == 5 and fwd(res=(0x40000, 60)) == 5 and fwd(res=(0x40000, 56)) == 4
+    assert fwd(cols=60) == 5 and fwd(rows=-1) == 4
+    bwd = lambda **k: _st(lambda: T.tp_dropout_bwd(k.get("d", D(0.1, 1)), k.get("dy", (0x10000, 64)), k.get("dx", (0x20000, 64)), k.get("pre"), k.get("db"),
+                                                   k.get("rows", 4096), k.get("cols", 64), k.get("ws"), stream=0))
+    assert bwd(d=D(1.5, 1)) == 2 and bwd(dy=(0, 64)) == 1 and bwd(dx=(0, 64)) == 1
+    assert bwd(dy=(0x10008, 64)) == 5 and bwd(pre=(0x30008, 64)) == 5 and bwd(db=0x40004) == 5 and bwd(cols=12) == 5
+    assert bwd(dy=(0x10000, 56)) == 4 and bwd(dx=(0x20000, 56)) == 4 and bwd(pre=(0x30000, 56)) == 4 and bwd(rows=-1) == 4
+    assert T.tp_bias_grad_workspace_size(4096, 64) > 16
+    assert bwd(db=0x40000, ws=(0x50000, 16)) == 7 and bwd(db=0x40000, ws=(0x50008, 1 << 20)) == 7
+
+
+def test_tensors_the_kernel_could_not_follow_are_refused():
+    """Host tensors and tensors of another type, before anything is launched."""
+    f, h = torch.zeros(4, 64), torch.zeros(4, 64, dtype=torch.bfloat16)
+    for call in (lambda: T.tp_dropout_fwd(T.Dropout(0.1, 1), f, None, T.EPI_NONE, (0x20000, 64, 0), stream=0),
+                 lambda: T.tp_dropout_fwd(T.Dropout(0.1, 1), (0x10000, 64, 1), None, T.EPI_NONE, h, rows=4, cols=64, stream=0),
+                 lambda: T.tp_dropout_fwd(T.Dropout(0.1, 1, 0, torch.zeros(1, dtype=torch.int64)), (0x10000, 64, 1), None, T.EPI_NONE, (0x20000, 64, 0),
+                                          rows=4, cols=64, stream=0),
+                 lambda: T.tp_dropout_bwd(T.Dropout(0.1, 1), h, (0x20000, 64), stream=0)):
+        with pytest.raises(ValueError, match="not on the GPU"):
+            call()
+    with pytest.raises(ValueError):
+        T.tp_dropout_fwd((0.1, 1), (0x10000, 64, 1), None, T.EPI_NONE, (0x20000, 64, 0), rows=4, cols=64, stream=0)
+
+
+# ------------------------------------------------------------------------------------------------ on the GPU
+def _rand(rows, cols, dtype, seed, std=1.0, pad=0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return (torch.randn(rows, cols + pad, generator=g, device="cuda") * std).to(dtype)[:, :cols]
+
+
+def _mask(d, rows, cols):
+    return torch.from_numpy(keep_mask((d.p, d.seed, d.offset, d.row0, d.col0), rows, cols)).cuda()
+
+
+SIZES = [(1, 8), (1, 4096), (3, 24), (37, 136), (300, 1024), (513, 72), (2050, 264), (1, 65536)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("x_f32,y_f32,epi,res,pre", [(1, 0, 1, 1, 0), (1, 0, 2, 0, 1), (0, 0, 0, 1, 0), (0, 1, 2, 1, 1), (1, 1, 0, 0, 1), (0, 0, 1, 0, 0)])
+def test_forward(rows, cols, x_f32, y_f32, epi, res, pre):
+    d = T.Dropout(0.3, 0x123456789ABCDEF, 7 + (5 << 32), row0=17, col0=40)
+    x = _rand(rows, cols, torch.float32 if x_f32 else torch.bfloat16, 1, 2.0, pad=8)
+    bias = _rand(1, cols, torch.bfloat16, 2)[0].contiguous() if epi else None
+    r = _rand(rows, cols, torch.bfloat16, 3, pad=16) if res else None
+    y = torch.full((rows + 1, cols + 8), 9.0, dtype=torch.float32 if y_f32 else torch.bfloat16, device="cuda")
+    p = torch.full((rows + 1, cols + 8), 9.0, dtype=torch.bfloat16, device="cuda") if pre else None
+    T.tp_dropout_fwd(d, x, bias, epi, y[:rows, :cols], residual=r, preact=p[:rows, :cols] if pre else None)
+    a = x.double() + (bias.double() if epi else 0)
+    z = (gelu64(a) if epi == 2 else a) * factor(d.p)
+    z = torch.where(_mask(d, rows, cols), z, 0.0) + (r.double() if res else 0)
+    # the sum a (one rounding), the factor and its product (two), the residual (one): 4 steps of 2^-24 of at most |a| f + |r|; GeLU 3e-7 |a| f besides
+    work = (4 * 2.0 ** -24 + (4e-7 if epi == 2 else 0)) * float(a.abs().max() * factor(d.p) + (r.abs().max() if res else 0))
+    near(y[:rows, :cols], z, y.dtype, work)
+    assert (y[rows] == 9).all() and (y[:, cols:] == 9).all()
+    if pre:
+        near(p[:rows, :cols], a, torch.bfloat16, 2.0 ** -24 * float(a.abs().max()))
+        assert (p[rows] == 9).all() and (p[:, cols:] == 9).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", SIZES + [(0, 64), (5000, 8), (700, 2560), (1500, 16400)])
+@pytest.mark.parametrize("gelu,db,ws", [(0, 0, 0), (1, 0, 0), (0, 1, 1), (1, 1, 1), (1, 1, 0)])
+def test_backward(rows, cols, gelu, db, ws):
+    d = T.Dropout(0.45, 3, 2, row0=5, col0=8)
+    dy, a = _rand(rows, cols, torch.bfloat16, 4, pad=8), _rand(rows, cols, torch.bfloat16, 5, 1.5, pad=16) if gelu else None
+    dx = torch.full((rows + 1, cols + 8), 9.0, dtype=torch.bfloat16, device="cuda")
+    out = torch.full((cols + 8,), 9.0, device="cuda") if db else None
+    need = T.tp_bias_grad_workspace_size(rows, cols)
+    T.tp_dropout_bwd(d, dy, dx[:rows, :cols], preact=a, db=out[:cols] if db else None, workspace=torch.empty(max(need, 16), dtype=torch.uint8, device="cuda") if ws else None)
+    ref = dy.double() * factor(d.p) * (slope64(a.double()) if gelu else 1.0)
+    ref = torch.where(_mask(d, rows, cols), ref, 0.0)
+    big = float(ref.abs().max()) if rows else 0.0
+    work = (3 * 2.0 ** -24 + (1e-6 if gelu else 0)) * max(big, 1.0)
+    near(dx[:rows, :cols], ref, torch.bfloat16, work)
+    assert (dx[rows] == 9).all() and (dx[:, cols:] == 9).all()
+    if db:          # addends off by (3 2^-24 + 1e-6 with GeLU') |dy| f; chains of at most rows / 32 + 32 + 64 additions, half a step of the sum of magnitudes each
+        each = float((dy.double().abs() * factor(d.p)).sum(0).max()) if rows else 0.0
+        sums = float(ref.abs().sum(0).max()) if rows else 0.0
+        near(out[:cols], ref.sum(0), torch.float32, each * (3 * 2.0 ** -24 + (1e-6 if gelu else 0)) + sums * 2.0 ** -24 * (rows / 32 + 96))
+        assert (out[cols:] == 9).all()
+
+
+@pytest.mark.gpu
+def test_backward_is_the_gradient_of_forward():
+    """Differences of the forward in fp32 against the backward, on the same mask."""
+    rows, cols, d = 24, 64, T.Dropout(0.25, 11, 12)
+    x, dy = _rand(rows, cols, torch.bfloat16, 6), _rand(rows, cols, torch.bfloat16, 7)
+    zero = torch.zeros(cols, dtype=torch.bfloat16, device="cuda")
+    dx = torch.empty_like(dy)
+    T.tp_dropout_bwd(d, dy, dx, preact=x)
+    h = 2.0 ** -6
+    y = [torch.empty(rows, cols, device="cuda") for _ in range(2)]
+    for s, t in zip((1, -1), y):
+        T.tp_dropout_fwd(d, x.float() + s * h, zero, T.EPI_BIAS_GELU, t)
+    num = (y[0].double() - y[1].double()) / (2 * h) * dy.double()
+    # third derivative of GeLU below 1.6: h^2 / 6 of it; cancellation 2^-22 |y| / h; half a step of bf16
+    tol = dy.double().abs() * factor(d.p) * (1.6 * h * h / 6 + 2.0 ** -22 * 5 / h) + dx.double().abs() * 2.0 ** -8
+    assert ((num - dx.double()).abs() <= tol + 1e-6).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("p", [0.0, 1.0, 1 / 65536, 65535 / 65536])
+def test_ends_of_the_probability(p):
+    rows, cols, d = 64, 512, T.Dropout(p, 5, 6)
+    x = _rand(rows, cols, torch.bfloat16, 8)
+    y = torch.empty(rows, cols, device="cuda")
+    T.tp_dropout_fwd(d, x, None, T.EPI_NONE, y)
+    keep = _mask(d, rows, cols)
+    assert bool(keep.all()) == (p == 0) and (p < 1 or not keep.any())
+    near(y, torch.where(keep, x.double() * factor(p), 0.0), torch.float32, 2.0 ** -23 * 5 * factor(p))
+
+
+@pytest.mark.gpu
+def test_dropped_infinities_and_nans_are_zeros():
+    rows, cols, d = 16, 256, T.Dropout(0.5, 5, 6)
+    keep = _mask(d, rows, cols)
+    bad = torch.tensor([float("inf"), float("-inf"), float("nan"), torch.finfo(torch.bfloat16).min], device="cuda").repeat(cols // 4)
+    x = torch.where(keep, 1.0, bad).to(torch.bfloat16)
+    for epi in (T.EPI_NONE, T.EPI_BIAS_GELU):
+        y = torch.empty(rows, cols, device="cuda")
+        T.tp_dropout_fwd(d, x, torch.zeros(cols, dtype=torch.bfloat16, device="cuda") if epi else None, epi, y)
+        assert (y[~keep] == 0).all() and torch.isfinite(y).all() and (y[keep] > 0).all()
+    dx, db = torch.empty_like(x), torch.empty(cols, device="cuda")
+    T.tp_dropout_bwd(d, x, dx, preact=x, db=db)
+    assert (dx[~keep] == 0).all() and torch.isfinite(dx).all() and torch.isfinite(db).all()
+    # kept ones go through
+    T.tp_dropout_fwd(d, torch.where(keep, float("nan"), 1.0), None, T.EPI_NONE, y)
+    assert torch.isnan(y[keep]).all() and (y[~keep] == 0).all()
+
+
+@pytest.mark.gpu
+def test_any_partition_draws_the_same_mask():
+    """Blocks of a 2 x 3 grid, each with its own position, put together what the whole matrix gets; other seeds and offsets do not."""
+    rows, cols = 60, 240
+    x = torch.ones(rows, cols, dtype=torch.bfloat16, device="cuda")
+    whole, parts = torch.empty_like(x), torch.empty_like(x)
+    T.tp_dropout_fwd(T.Dropout(0.4, 21, 22), x, None, T.EPI_NONE, whole)
+    for i in range(2):
+        for j in range(3):
+            b = (slice(30 * i, 30 * i + 30), slice(80 * j, 80 * j + 80))
+            T.tp_dropout_fwd(T.Dropout(0.4, 21, 22, row0=30 * i, col0=80 * j), x[b], None, T.EPI_NONE, parts[b])
+    assert torch.equal(whole, parts)
+    for other in (T.Dropout(0.4, 22, 22), T.Dropout(0.4, 21, 23), T.Dropout(0.4, 21 + (1 << 40), 22), T.Dropout(0.4, 21, 22 + (1 << 40))):
+        T.tp_dropout_fwd(other, x, None, T.EPI_NONE, parts)
+        assert 0.3 < (parts != whole).float().mean() < 0.7
+
+
+@pytest.mark.gpu
+def test_far_positions_and_in_place():
+    d = T.Dropout(0.5, (1 << 64) - 1, (1 << 64) - 1, row0=(1 << 32) - 40, col0=(1 << 35) - 128)
+    x = _rand(40, 128, torch.bfloat16, 9)
+    ref = torch.where(_mask(d, 40, 128), x.double() * 2, 0.0)
+    res = x.clone()
+    T.tp_dropout_fwd(d, x.float(), None, T.EPI_NONE, res, residual=res)
+    near(res, ref + x.double(), torch.bfloat16, 1e-6)
+    y = x.float()
+    T.tp_dropout_fwd(d, y, None, T.EPI_NONE, y)
+    near(y, ref, torch.float32)
+    T.tp_dropout_bwd(d, x, x)
+    near(x, ref, torch.bfloat16)
+
+
+@pytest.mark.gpu
+def test_captured_graph_draws_a_new_mask_each_replay():
+    """The offset's device part is read when the kernels run; another stream than the tensors' own; replays against eager calls."""
+    rows, cols = 128, 512
+    x, dy = _rand(rows, cols, torch.bfloat16, 10), _rand(rows, cols, torch.bfloat16, 11)
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    d = T.Dropout(0.3, 77, 1000, step)
+    y, dx, db = torch.empty_like(x), torch.empty_like(x), torch.empty(cols, device="cuda")
+    ws = torch.empty(max(16, T.tp_bias_grad_workspace_size(rows, cols)), dtype=torch.uint8, device="cuda")
+
+    def both():
+        T.tp_dropout_fwd(d, x, None, T.EPI_NONE, y, residual=dy)
+        T.tp_dropout_bwd(d, dy, dx, preact=x, db=db, workspace=ws)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        both()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        both()
+        step += 1
+    step.zero_()
+    for i in range(4):
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (y, dx, db)]
+        e = [torch.empty_like(t) for t in (y, dx, db)]
+        here = T.Dropout(0.3, 77, 1000 + i)
+        T.tp_dropout_fwd(here, x, None, T.EPI_NONE, e[0], residual=dy)
+        T.tp_dropout_bwd(here, dy, e[1], preact=x, db=e[2], workspace=ws)
+        for a, b in zip(got, e):
+            assert torch.equal(a, b), i
+    # an offset that wraps around
+    step.fill_(-1)
+    T.tp_dropout_fwd(T.Dropout(0.3, 77, 3, step), x, None, T.EPI_NONE, y)
+    T.tp_dropout_fwd(T.Dropout(0.3, 77, 2), x, None, T.EPI_NONE, dx)
+    assert torch.equal(y, dx)
