@@ -347,6 +347,71 @@ int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_
 int tp_dropout_bwd(const tp_dropout_t* drop, const void* dy, int64_t ld_dy, const void* preact, int64_t ld_pre, void* dx, int64_t ld_dx,
                    void* db_f32, int64_t rows, int64_t cols, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Low-rank adapters of many requests beside the shared projection of tp_linear_fwd.  A pool holds n_adapters adapters of one rank (a smaller one is
+ * filled up with zero rows); adapter i has the factors A_i: [rank, H] and B_i: [rank, F], bf16, both as `rank` rows, and the scale s_i.  The rows of
+ * a block come in segments, a request each: segment s is rows offsets[s] .. offsets[s + 1] - 1 and uses adapter ids[s], or none where ids[s] is not one
+ * of 0 .. n_adapters - 1.  Rows in no segment (before offsets[0], behind the last one) are left as they were in every output.  All three arrays are read
+ * by the kernels: lengths may differ from call to call, and from replay to replay of a captured graph.  offsets must ascend (empty
+ * segments are fine); values outside 0 .. rows are taken as the nearest of these, and from any others come wrong rows, but no access outside the blocks.
+ *   offsets : DEVICE int32 [n_segments + 1];   ids : DEVICE int32 [n_segments];   scale : DEVICE fp32 [n_adapters] or NULL (all 1);
+ *   rank    : a multiple of 8 up to TP_ADAPTER_MAX_RANK.
+ */
+#define TP_ADAPTER_MAX_RANK 128
+#define TP_ADAPTER_MAX_POOL 32767
+typedef struct { const int32_t* offsets; const int32_t* ids; const float* scale; int32_t n_segments, n_adapters, rank; } tp_adapters_t;
+/* A chunk of one factor of every adapter: bf16, adapter i's [rank, cols] chunk at ptr + i stride, its rows ld apart (both in elements). */
+typedef struct { const void* ptr; int64_t ld, stride; } tp_factor_t;
+/* The same as an output: fp32. */
+typedef struct { void* ptr; int64_t ld, stride; } tp_factor_out_t;
+
+/*
+ * tp_adapter_fwd -- the adapters' part of a rank's forward share, and what follows it:
+ *     V = sum_{k<n_steps} drop(X_k) A_k^T   (row by row, with the row's own adapter),   A = c + s V B + bias,   y = GeLU(A) (TP_EPI_BIAS_GELU) or A
+ *   grid, dims, n_steps, x_blocks : as in tp_linear_fwd: X_k is [m, k].
+ *   a_blocks : host array [n_steps]: A_k is the chunk [rank, k] of A's columns that belongs to X_k (chunk a_col[k] of tp_block_map).
+ *   b        : the chunk [rank, n] of B's columns (chunk out_col).
+ *   drop     : dropout on the adapters' input, or NULL.  Positions are those in the full X [M, H] (the library adds the blocks' own), behind
+ *              row0, col0.
+ *   c, y     : [m, n], fp32 or bf16 each: the shared product (tp_linear_fwd with TP_EPI_NONE) and the output.  y may be c itself (same address, type and
+ *              leading dimension), else the two must not overlap (TP_ERR_SHAPE).   bias, epi, preact: as in tp_linear_fwd.
+ *   v        : optional fp32 [m, rank], rows rank apart: V, saved for backward (rows without an adapter are not written).
+ *   workspace: >= tp_adapter_workspace_size(.., TP_PASS_FWD, ..) bytes, 16-byte aligned.
+ * V is the rank's own sum.  Where the shared product is an additive partial (1D_ROW, 3D_GATHERED), so is this: every rank adds the part of its own
+ * columns of A, the reduction that completes c completes it, and epi, preact and a bf16 y are refused as in tp_linear_fwd.
+ * Defined by: the adapted layer X (W + s A^T B) under the partition of tp_linear_fwd (Section 2.2): A is cut like W's rows, B like W's columns.
+ * V is fp32; in the second product it stands as a sum of bf16 terms that is off by 2^-17 (bf16 y) or 2^-25 (fp32 y) of it.
+ * Errors: TP_ERR_NULL, TP_ERR_MODE, TP_ERR_GRID, TP_ERR_SHAPE (also: rank, pool or segment counts out of range), TP_ERR_ALIGN, TP_ERR_DTYPE,
+ * TP_ERR_WORKSPACE, TP_ERR_HIP; nothing is launched unless every check has passed.
+ */
+int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, const tp_adapters_t* adapters, const tp_cblk_t* x_blocks,
+                   const tp_factor_t* a_blocks, const tp_factor_t* b, const tp_dropout_t* drop, tp_oblk_t c, const void* bias, int epi, tp_oblk_t y,
+                   tp_oblk_t preact, float* v, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * tp_adapter_bwd -- the gradients of the adapters' part, each only if wanted:
+ *     U = sum_{k<n_steps} dY_k B_k^T,   dX = dx_base + drop'(s U A),   dA_i = s_i sum U^T drop(X),   dB_i = s_i sum V^T dY   (sums over the rows of adapter i)
+ *   n_steps, dy_blocks, b_blocks : dY_k [m, F chunk] and the chunk [rank, F chunk] of B that belongs to it, in the order of TP_PASS_DX's a blocks
+ *              (needed for dX and dA).   dY is the gradient of A = c + s V B + bias.
+ *   a        : the chunk [rank, n_dx] of A's columns that TP_PASS_DX's output has (needed for dX).
+ *   dx_base, dx : [m, n_dx], fp32 or bf16 each: the shared product's dX (tp_linear_bwd) and the output; dx may be dx_base itself, as y and c above.
+ *   x_own    : the rank's own X block [m, n_dx] (needed for dA);   dy_own: its own dY block [m, n_fwd] and v: V of these rows (needed for dB).
+ *   da, db   : fp32, [rank, n_dx] and [rank, n_fwd] per adapter.  Adapters without rows get zeros.  accumulate != 0: added to what is there.
+ *   drop     : as in forward (NULL: none).   workspace: >= tp_adapter_workspace_size(.., TP_PASS_DX, ..) bytes.
+ * dA and dB are the sums over this rank's own rows: additive partials over the row chunks, and, where U or V is one (1D_COL, 1D_ROW, 3D_GATHERED), over those
+ * ranks as well.  A dX that the map marks as a partial must be fp32.  The order of every sum is fixed by the arguments.  Apart from dx over dx_base no
+ * output may overlap an input or another output.
+ * Defined by: the gradients of tp_adapter_fwd under the same partition.  Errors: as tp_adapter_fwd.
+ */
+int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, const tp_adapters_t* adapters, const tp_cblk_t* dy_blocks,
+                   const tp_factor_t* b_blocks, const tp_factor_t* a, const tp_dropout_t* drop, tp_oblk_t dx_base, tp_oblk_t dx, const tp_cblk_t* x_own,
+                   tp_factor_out_t da, const tp_cblk_t* dy_own, const float* v, tp_factor_out_t db, int accumulate, void* workspace,
+                   size_t workspace_bytes, void* hip_stream);
+
+/* Bytes of device workspace tp_adapter_fwd (TP_PASS_FWD) or tp_adapter_bwd (TP_PASS_DX) may need: planes of V or U, and of dA and dB where their rows
+ * are shared out.  Only n_segments, n_adapters and rank of `adapters` are looked at.  0 on invalid arguments.  Host only. */
+size_t tp_adapter_workspace_size(const tp_grid_t* grid, const tp_dims_t* dims, int pass, const tp_adapters_t* adapters);
+
 /* Human-readable name of a status code (static storage). */
 const char* tp_strerror(int status);
 

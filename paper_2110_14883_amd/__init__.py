@@ -6,4 +6,5 @@ from .binding import (  # noqa: F401
     PASS_DW, PASS_DW_PARTIALS, PASS_DX, PASS_DX_PARTIALS, PASS_FWD, Grid, TpError, lib, tp_block_map, tp_dgelu, tp_linear_bwd,
     tp_linear_fwd, tp_linear_workspace_size, tp_bias_act, tp_linear_bwd_partials, tp_partials_map, tp_bias_grad, plan_opts, tp_strerror,
     tp_linear_fwd_static, tp_static_scratch_bytes, tp_bias_grad_workspace_size, Dropout, tp_dropout_fwd, tp_dropout_bwd,
+    Adapters, tp_adapter_fwd, tp_adapter_bwd, tp_adapter_workspace_size,
 )

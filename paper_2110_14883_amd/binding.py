@@ -64,6 +64,25 @@ class Dropout(NamedTuple):
     col0: int = 0
 
 
+class _AdaptersS(C.Structure):
+    _fields_ = [("offsets", C.c_void_p), ("ids", C.c_void_p), ("scale", C.c_void_p), ("n_segments", C.c_int32), ("n_adapters", C.c_int32), ("rank", C.c_int32)]
+
+
+class _Factor(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("ld", C.c_int64), ("stride", C.c_int64)]
+
+
+class Adapters(NamedTuple):
+    """Which rows use which adapter of a pool (tp_adapters_t): int32 device tensors offsets [n_segments + 1] and ids [n_segments] (an id outside the pool:
+    none), and the adapters' scales (fp32 device tensor, None: all 1).  The factors are tensors [n_adapters, rank, cols]."""
+    offsets: Any
+    ids: Any
+    n_adapters: int
+    rank: int
+    scale: Any = None
+    n_segments: Any = None
+
+
 class _PlanOpts(C.Structure):
     _fields_ = [("tile", C.c_int), ("split_k", C.c_int), ("group_m", C.c_int), ("rotate", C.c_int), ("trim", C.c_int)]
 
@@ -171,6 +190,15 @@ def lib() -> C.CDLL:
         L.tp_dropout_bwd.restype = C.c_int
         L.tp_dropout_bwd.argtypes = [dp, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64,
                                      C.c_void_p, C.c_size_t, C.c_void_p]
+        ap, fp, gp, cp = C.POINTER(_AdaptersS), C.POINTER(_Factor), C.POINTER(_GridS), C.POINTER(_CBlk)
+        L.tp_adapter_fwd.restype = C.c_int
+        L.tp_adapter_fwd.argtypes = [gp, C.POINTER(_DimsS), C.c_int, ap, cp, fp, fp, dp, _OBlk, C.c_void_p, C.c_int, _OBlk, _OBlk, C.c_void_p, C.c_void_p,
+                                     C.c_size_t, C.c_void_p]
+        L.tp_adapter_bwd.restype = C.c_int
+        L.tp_adapter_bwd.argtypes = [gp, C.POINTER(_DimsS), C.c_int, ap, cp, fp, fp, dp, _OBlk, _OBlk, cp, _Factor, cp, C.c_void_p, _Factor, C.c_int,
+                                     C.c_void_p, C.c_size_t, C.c_void_p]
+        L.tp_adapter_workspace_size.restype = C.c_size_t
+        L.tp_adapter_workspace_size.argtypes = [gp, C.POINTER(_DimsS), C.c_int, ap]
         L.tp_strerror.restype = C.c_char_p
         L.tp_strerror.argtypes = [C.c_int]
         _lib = L
@@ -188,20 +216,22 @@ def _call():
     spec.loader.exec_module(m)
     try:
         import torch
-        dtypes, device = (torch.float32, torch.bfloat16), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        dtypes, int32, device = (torch.float32, torch.bfloat16), torch.int32, getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     except ImportError:                      # blocks are then (address, leading dimension[, dtype]) sequences
-        dtypes, device = (None, None), None
+        dtypes, int32, device = (None, None), None, None
     names = ("tp_linear_fwd_ex", "tp_linear_fwd_static", "tp_linear_bwd_ex", "tp_linear_bwd_partials_ex", "tp_bias_act", "tp_dgelu",
              "tp_bias_grad")
     m.bind(*[C.cast(getattr(L, n), C.c_void_p).value for n in names], *dtypes)
-    m.bind_ops(*[C.cast(getattr(L, n), C.c_void_p).value for n in ("tp_dropout_fwd", "tp_dropout_bwd")], device)
+    ops = ("tp_dropout_fwd", "tp_dropout_bwd", "tp_adapter_fwd", "tp_adapter_bwd")
+    m.bind_ops(*[C.cast(getattr(L, n), C.c_void_p).value for n in ops], int32, device)
     return m
 
 
 EXPORTS = ("tp_block_map", "tp_linear_workspace_size", "tp_linear_workspace_size_ex", "tp_linear_fwd", "tp_linear_fwd_ex",
            "tp_linear_bwd", "tp_linear_bwd_ex", "tp_dgelu", "tp_partials_map", "tp_linear_bwd_partials",
            "tp_linear_bwd_partials_ex", "tp_bias_act", "tp_bias_grad", "tp_strerror", "tp_linear_fwd_static",
-           "tp_static_scratch_bytes", "tp_bias_grad_workspace_size", "tp_dropout_fwd", "tp_dropout_bwd")
+           "tp_static_scratch_bytes", "tp_bias_grad_workspace_size", "tp_dropout_fwd", "tp_dropout_bwd",
+           "tp_adapter_fwd", "tp_adapter_bwd", "tp_adapter_workspace_size")
 
 
 # ----------------------------------------------------------------------------- marshalling helpers
@@ -346,3 +376,23 @@ def tp_dropout_bwd(dropout: Dropout, dy, dx, preact=None, db=None, rows: int | N
     """dx = drop'(dy) GeLU'(preact); db: its column sums (workspace: as tp_bias_grad)."""
     rows, cols = _rows_cols(dy, rows, cols)
     _check(_call().dropout_bwd(dropout, dy, preact, dx, db, rows, cols, workspace, _stream(stream)), "tp_dropout_bwd")
+
+
+def tp_adapter_workspace_size(grid: Grid, dims, pass_: int, adapters: Adapters) -> int:
+    n = adapters.n_segments if adapters.n_segments is not None else adapters.ids.numel()
+    g, d, a = grid._c(), _dims(dims), _AdaptersS(None, None, None, int(n), int(adapters.n_adapters), int(adapters.rank))
+    return int(lib().tp_adapter_workspace_size(C.byref(g), C.byref(d), int(pass_), C.byref(a)))
+
+
+def tp_adapter_fwd(grid: Grid, dims, n_steps: int, adapters: Adapters, x_blocks, a_blocks, b, c, bias, epi: int, y, preact=None, v=None,
+                   dropout: Dropout | None = None, workspace=None, stream=None) -> None:
+    """y = act(c + s (sum_k drop(X_k) A_k^T) B + bias), every row with its own adapter."""
+    _check(_call().adapter_fwd(grid._at(), dims, n_steps, adapters, x_blocks, a_blocks, b, dropout, c, bias, epi, y, preact, v, workspace,
+                               _stream(stream)), "tp_adapter_fwd")
+
+
+def tp_adapter_bwd(grid: Grid, dims, n_steps: int, adapters: Adapters, dy_blocks=None, b_blocks=None, a=None, dx_base=None, dx=None, x_own=None, da=None,
+                   dy_own=None, v=None, db=None, dropout: Dropout | None = None, accumulate: bool = False, workspace=None, stream=None) -> None:
+    """dx = dx_base + drop'(s U A) with U = sum_k dY_k B_k^T;  da = s U^T drop(X);  db = s V^T dY: each only if its output is given."""
+    _check(_call().adapter_bwd(grid._at(), dims, n_steps, adapters, dy_blocks, b_blocks, a, dropout, dx_base, dx, x_own, da, dy_own, v, db,
+                               int(accumulate), workspace, _stream(stream)), "tp_adapter_bwd")

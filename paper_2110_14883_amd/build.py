@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libtplinear.so")
 PROBE_LIB_PATH = os.path.join(PKG_DIR, "libtpprobe.so")      # bench-only measurement aid (tp_probe.hip)
 CALL_LIB_PATH = os.path.join(PKG_DIR, "_tpcall" + importlib.machinery.EXTENSION_SUFFIXES[0])
 CALL_SOURCE = "tp_pycall.cpp"
-SOURCES = ["tp_kernels.hip", "tp_gemm4.hip", "tp_gemm_ms.hip", "tp_small.hip", "tp_dropout.hip", "tp_api.cpp", "tp_ops.cpp"]
+SOURCES = ["tp_kernels.hip", "tp_gemm4.hip", "tp_gemm_ms.hip", "tp_small.hip", "tp_dropout.hip", "tp_adapter.hip", "tp_api.cpp", "tp_ops.cpp"]
 PROBE_SOURCE = "tp_probe.hip"
 HEADERS = [os.path.join(ROOT, "include", h) for h in ("tp_linear.h", "tp_probe.h")] + [
     os.path.join(CSRC, h) for h in ("tp_internal.h", "tp_checks.h", "tp_device.h", "tp_stream.h", "tp_random.h")]

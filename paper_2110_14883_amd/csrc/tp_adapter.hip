@@ -1,0 +1,517 @@
+// gfx950 (MI355X, CDNA4): low-rank adapters of many requests beside a shared projection (paper Section 2.2: the projection is a rank's share of the
+// linear layer).  With the factors A_i: [rank, H], B_i: [rank, F] and scale s_i of a row's adapter i
+//   forward   V = drop(X) A_i^T,   Y = act(C + s_i V B_i + bias)
+//   backward  U = dY B_i^T,        dX = dX_base + drop'(s_i U A_i),    dA_i = s_i U^T drop(X),   dB_i = s_i V^T dY
+// Both factors lie as `rank` long rows, so forward and backward are the same three products:
+//   down  [rows, K] x [rank, K]^T      both operands contraction-contiguous: fragments straight from memory
+//   up    [rows, rank] x [rank, cols]  the factor's 8 x 8 blocks transposed in registers
+//   grad  [rows, rank]^T x [rows, cols]
+// All three are bound by memory: the rank is at most 128, so a row of X or Y that is read takes 2 to 64 flops a byte.  V and U stay in fp32.  Where they
+// are a matrix operand they go in as a sum of bf16 terms, two (2^-17) for bf16 results and three (2^-25) for fp32 ones: the matrix
+// unit has the time, and rounding them once would cost a bf16 step of the adapters' part.
+//
+// Rows come in segments, a request each, described by device arrays.  A workgroup works on a tile of one segment's rows: it finds its tile from
+// the offsets itself (one trip to memory for up to 64 segments), so a call is the same launches whatever the lengths, and can be captured.  Offsets are
+// clamped to the rows there are and an adapter that the pool does not have is none: bad ones give wrong rows, never a wild access.
+#include "tp_random.h"
+
+namespace tpl {
+
+namespace {
+
+__device__ __forceinline__ float as_float(uint32_t w) { return __builtin_bit_cast(float, w); }   // (of a value: a bit cast of a vector's element takes its first one)
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// inclusive sum over the wave's lanes
+__device__ __forceinline__ int wave_sums(int x, int l) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(x, d);
+        if (l >= d) x += o;
+    }
+    return x;
+}
+// rows [lo, lo + len) of segment i, clamped
+__device__ __forceinline__ void segment(const SegArgs& s, int i, int& lo, int& len) {
+    lo = len = 0;
+    if (i < s.n) {
+        lo = s.offsets[i];
+        int hi = s.offsets[i + 1];
+        lo = lo < 0 ? 0 : lo > s.rows ? s.rows : lo;
+        hi = hi < 0 ? 0 : hi > s.rows ? s.rows : hi;
+        len = hi > lo ? hi - lo : 0;
+    }
+}
+__device__ __forceinline__ int adapter(const SegArgs& s, int i) {      // -1: none
+    const int id = s.ids[i];
+    return id >= 0 && id < s.pool ? id : -1;
+}
+
+struct Tile { int row0, rows, id; };
+// tile t of the tiles of at most T rows that the segments have, in their order; the same for every lane of a wave
+__device__ __forceinline__ bool find_tile(const SegArgs& s, int t, int T, Tile& out) {
+    const int l = threadIdx.x & 63;
+    int base = 0;
+    for (int first = 0; first < s.n; first += 64) {
+        int lo, len;
+        segment(s, first + l, lo, len);
+        const int count = (len + T - 1) / T, sums = wave_sums(count, l);
+        const uint64_t behind = __ballot(base + sums > t);
+        if (behind) {
+            const int j = __builtin_ctzll(behind);
+            const int at = __builtin_amdgcn_readlane(lo, j), end = at + __builtin_amdgcn_readlane(len, j);
+            out.row0 = at + (t - base - (__builtin_amdgcn_readlane(sums, j) - __builtin_amdgcn_readlane(count, j))) * T;
+            out.rows = end - out.row0 < T ? end - out.row0 : T;
+            out.id = uni(adapter(s, first + j));
+            return out.row0 >= at && out.rows > 0;               // (not so only where sums of wild offsets overflow)
+        }
+        base += __builtin_amdgcn_readlane(sums, 63);
+    }
+    return false;
+}
+
+// 8 values -> their bf16 terms: v = t[0] + t[1] (+ t[2]); an infinity is its first term alone
+template <int N>
+__device__ __forceinline__ void split_terms(const float (&v)[8], u32x4_t (&t)[N]) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = v[i];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            t[n][i] = pack_bf16(r[2 * i], r[2 * i + 1]);
+            if (n + 1 < N) {
+                const float a = r[2 * i] - bf16_lo(t[n][i]), b = r[2 * i + 1] - bf16_hi(t[n][i]);
+                r[2 * i] = a == a ? a : 0.0f;
+                r[2 * i + 1] = b == b ? b : 0.0f;
+            }
+        }
+    }
+}
+// 8 x 8 block: in[j] is row j of eight columns -> out[e] is column e of eight rows
+__device__ __forceinline__ void transpose8(const u32x4_t (&in)[8], u32x4_t (&out)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[e][i] = __builtin_amdgcn_perm(in[2 * i + 1][e >> 1], in[2 * i][e >> 1], sel);
+    }
+}
+__device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, const f32x4_t& c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// ---------------------------------------------------------------------------------------------
+// down.  A tile of 16 MT rows by all 16 RB ranks; the eight waves of a workgroup, and the workgroups of a tile, share K in units of 64 (32 where
+// registers would not hold two units), and the waves' sums meet in LDS in their order.  A wave keeps the next unit's loads in flight.
+// ---------------------------------------------------------------------------------------------
+constexpr int DOWN_WAVES = 8;
+template <int MT, int RB, bool DROP>
+__global__ __launch_bounds__(64 * DOWN_WAVES) void tp_adapter_down_kernel(const DownArgs p) {
+    constexpr int H = MT + RB >= 8 ? 1 : 2;                             // k steps of 32 in a unit
+    __shared__ __attribute__((aligned(16))) float part[DOWN_WAVES][16][16 * RB + 4];
+    Tile t;
+    if (!find_tile(p.seg, blockIdx.x, 16 * MT, t) || t.id < 0) return;
+    const int l = threadIdx.x & 63, c = l & 15, g = l >> 4, w = uni(threadIdx.x >> 6);
+    const int KT = (p.K + 32 * H - 1) / (32 * H), total = p.n_steps * KT, shares = p.splits * DOWN_WAVES, share = blockIdx.y * DOWN_WAVES + w;
+    int u = uni((int)((int64_t)total * share / shares));
+    const int end = uni((int)((int64_t)total * (share + 1) / shares));
+    int step = uni(u / KT), kt = u - step * KT;
+    Mask m;
+    if constexpr (DROP) m = open_mask(p.drop);
+    struct Unit { u32x4_t x[H][MT], f[H][RB]; uint32_t group; };
+    auto fetch = [&](Unit& n) __attribute__((always_inline)) {           // the unit at (step, kt), which moves on
+        const int ldp = p.ldp[step], ldf = p.ldf[step];
+        const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const uint16_t*>(p.p[step]) + (int64_t)t.row0 * ldp, ((int64_t)(t.rows - 1) * ldp + p.K) * 2);
+        const __amdgpu_buffer_rsrc_t rf = make_rsrc(static_cast<const uint16_t*>(p.f[step]) + t.id * p.strides[step], ((int64_t)(p.rank - 1) * ldf + p.K) * 2);
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            const int k = 32 * (H * kt + h) + 8 * g;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) n.x[h][i] = buf_load16(rx, k < p.K ? (uint32_t)(((16 * i + c) * ldp + k) * 2) : OOB_OFFSET);
+#pragma unroll
+            for (int j = 0; j < RB; ++j) n.f[h][j] = buf_load16(rf, k < p.K ? (uint32_t)(((16 * j + c) * ldf + k) * 2) : OOB_OFFSET);
+        }
+        if constexpr (DROP) n.group = p.group0[step] + 4 * H * kt + g;
+        if (++kt == KT) { kt = 0; ++step; }
+    };
+    f32x4_t acc[MT][RB];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < RB; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    auto multiply = [&](Unit& n) __attribute__((always_inline)) {        // acc[i][j][e]: row 16 i + c, rank 16 j + 4 g + e
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                u32x4_t x = n.x[h][i];
+                if constexpr (DROP) x = clear_dropped(m, draw(m, n.group + 4 * h, p.drop.row0 + (uint32_t)(t.row0 + 16 * i + c)), x);
+#pragma unroll
+                for (int j = 0; j < RB; ++j) acc[i][j] = mfma(n.f[h][j], x, acc[i][j]);
+            }
+    };
+    if (u < end) {
+        Unit a, b;
+        fetch(a);
+        while (true) {
+            if (u + 1 < end) fetch(b);
+            multiply(a);
+            if (++u >= end) break;
+            if (u + 1 < end) fetch(a);
+            multiply(b);
+            if (++u >= end) break;
+        }
+    }
+    float* const out = p.out + blockIdx.y * p.plane;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        if (i) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < RB; ++j) *reinterpret_cast<f32x4_t*>(&part[w][c][16 * j + 4 * g]) = acc[i][j];
+        __syncthreads();
+        const int row = threadIdx.x / (4 * RB), q = threadIdx.x % (4 * RB);
+        if (row < 16 && 16 * i + row < t.rows && 4 * q < p.rank) {
+            f32x4_t s = *reinterpret_cast<const f32x4_t*>(&part[0][row][4 * q]);
+#pragma unroll
+            for (int v = 1; v < DOWN_WAVES; ++v) s += *reinterpret_cast<const f32x4_t*>(&part[v][row][4 * q]);
+            if constexpr (DROP) s *= p.drop.factor;
+            *reinterpret_cast<f32x4_t*>(out + (int64_t)(t.row0 + 16 * i + row) * p.rank + 4 * q) = s;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// up.  A wave has a strip of 128 columns of a tile's rows: it turns the strip of its adapter's factor into matrix operands once, eight 16-column
+// blocks whose columns are 8 c + j, so that a lane ends up with eight neighbouring columns of four rows: whole 16-byte pieces of C and Y,
+// and one draw a row.
+// GP: groups of eight ranks (2: up to 16 ranks, where both halves of the wave's k range hold the same ranks and the terms of V lie
+// side by side in it; 4, 8, 16: up to 32, 64, 128 ranks).
+// ---------------------------------------------------------------------------------------------
+template <int GP, int TERMS, bool DROP>
+__global__ __launch_bounds__(256) void tp_adapter_up_kernel(const UpArgs p) {
+    constexpr int NS = GP >= 4 ? GP / 4 : 1;
+    const int l = threadIdx.x & 63, c = l & 15, g = l >> 4;
+    const int strip = uni(blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6));
+    if (strip * 128 >= p.cols) return;
+    Tile t;
+    if (!find_tile(p.seg, blockIdx.x, p.tile, t)) return;
+    const int n = strip * 128 + 8 * c;
+    const bool in = n < p.cols;
+    auto group = [&](int s) __attribute__((always_inline)) { return GP >= 4 ? 4 * s + g : g & (GP - 1); };
+    u32x4_t f[NS][8];
+    float scale = 1.0f;
+    if (t.id >= 0) {
+        if (p.scale) scale = p.scale[t.id];
+        const __amdgpu_buffer_rsrc_t rf = make_rsrc(static_cast<const uint16_t*>(p.f) + t.id * p.stride, ((int64_t)(p.rank - 1) * p.ldf + p.cols) * 2);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            u32x4_t rows[8];
+            const bool ok = in && 8 * group(s) < p.rank;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) rows[j] = buf_load16(rf, ok ? (uint32_t)(((8 * group(s) + j) * p.ldf + n) * 2) : OOB_OFFSET);
+            transpose8(rows, f[s]);
+        }
+    }
+    Mask m;
+    if constexpr (DROP) m = open_mask(p.drop);
+    float b[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (p.bias && in) {
+        const u32x4_t q = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(p.bias) + n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { b[2 * i] = bf16_lo(q[i]); b[2 * i + 1] = bf16_hi(q[i]); }
+    }
+    for (int r0 = 0; r0 < t.rows; r0 += 16) {
+        // C of rows r0 + 4 g + e (past the end: the last row; past the columns: the first ones)
+        u32x4_t cv[4][2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = r0 + 4 * g + e < t.rows ? r0 + 4 * g + e : t.rows - 1;
+            const int64_t at = (int64_t)(t.row0 + r) * p.ldc + (in ? n : 0);
+            if (p.c_f32) {
+                const u32x4_t* const src = reinterpret_cast<const u32x4_t*>(static_cast<const float*>(p.c) + at);
+                cv[e][0] = __builtin_nontemporal_load(src);
+                cv[e][1] = __builtin_nontemporal_load(src + 1);
+            } else {
+                cv[e][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(p.c) + at));
+                cv[e][1] = cv[e][0];
+            }
+        }
+        f32x4_t acc[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (t.id >= 0) {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (r0 + c < t.rows && 8 * group(s) < p.rank) {
+                    const int64_t at = (int64_t)(t.row0 + r0 + c) * p.rank + 8 * group(s);
+                    for (int z = 0; z < p.splits; ++z) {
+                        const f32x4_t *src = reinterpret_cast<const f32x4_t*>(p.v + z * p.plane + at), lo = src[0], hi = src[1];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { v[i] += lo[i]; v[4 + i] += hi[i]; }
+                    }
+                    if (p.v_out && strip == 0 && (GP >= 4 || g < GP)) {
+                        f32x4_t* const to = reinterpret_cast<f32x4_t*>(p.v_out + at);
+                        to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+                        to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= scale;
+                u32x4_t term[TERMS];
+                split_terms(v, term);
+                if constexpr (GP >= 4) {
+#pragma unroll
+                    for (int q = 0; q < TERMS; ++q)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) acc[j] = mfma(term[q], f[s][j], acc[j]);
+                } else {
+                    const bool second = g >= 2;
+                    u32x4_t both;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) both[i] = second ? term[1][i] : term[0][i];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[j] = mfma(both, f[s][j], acc[j]);
+                    if constexpr (TERMS == 3) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) both[i] = second ? 0u : term[2][i];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) acc[j] = mfma(both, f[s][j], acc[j]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = r0 + 4 * g + e;
+            float v[8];
+            if (p.c_f32) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = as_float(cv[e][j >> 2][j & 3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = j & 1 ? bf16_hi(cv[e][0][j >> 1]) : bf16_lo(cv[e][0][j >> 1]);
+            }
+            if constexpr (DROP) {
+                const u32x4_t bits = draw(m, p.drop.group0 + (uint32_t)(n >> 3), p.drop.row0 + (uint32_t)(t.row0 + r));
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += keeps(m, bits, j) ? acc[j][e] * p.drop.factor : 0.0f;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += acc[j][e];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += b[j];
+            if (r >= t.rows || !in) continue;
+            const int64_t row = t.row0 + r;
+            if (p.pre) {
+                const u32x4_t s = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+                __builtin_nontemporal_store(s, reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(p.pre) + row * p.ldp + n));
+            }
+            if (p.gelu) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = gelu_f(v[j]);
+            }
+            if (p.out_f32) {
+                f32x4_t* const to = reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + row * p.ldo + n);
+                __builtin_nontemporal_store(f32x4_t{v[0], v[1], v[2], v[3]}, to);
+                __builtin_nontemporal_store(f32x4_t{v[4], v[5], v[6], v[7]}, to + 1);
+            } else {
+                const u32x4_t o = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+                __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n));
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// grad.  A workgroup has a strip of 128 columns, 16 RB ranks and a share of an adapter's rows, counted in units of 32 rows of one segment; its four
+// waves take the units in turn and their sums meet in LDS in order.  The factor's layout again leaves a lane with eight neighbouring columns.  With several
+// shares their sums go to planes that a second kernel adds in order: nothing depends on which workgroup runs first.
+// ---------------------------------------------------------------------------------------------
+constexpr int GRAD_WAVES = 4;
+template <int RB>
+__global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const GradArgs p, const int strips0, const int strips) {
+    __shared__ __attribute__((aligned(16))) float part[GRAD_WAVES][16][132];
+    const int l = threadIdx.x & 63, c = l & 15, g = l >> 4, w = uni(threadIdx.x >> 6);
+    const int chunks = (p.rank + 16 * RB - 1) / (16 * RB);
+    int x = blockIdx.x;
+    const int strip_all = x % strips; x /= strips;
+    const int rank0 = (x % chunks) * 16 * RB; x /= chunks;
+    const int share = x % p.shares, a = x / p.shares;
+    const int which = strip_all >= strips0, strip = which ? strip_all - strips0 : strip_all;
+    const GradSide& q = p.side[which];
+    const int n = strip * 128 + 8 * c;
+    const bool in = n < q.cols;
+    // units of this adapter, those of this share
+    int total = 0;
+    for (int first = 0; first < p.seg.n; first += 64) {
+        int lo, len;
+        segment(p.seg, first + l, lo, len);
+        const int count = len > 0 && adapter(p.seg, first + l) == a ? (len + 31) / 32 : 0;
+        total += __builtin_amdgcn_readlane(wave_sums(count, l), 63);
+    }
+    if (p.shares > 1 && share == 0 && strip_all == 0 && rank0 == 0 && threadIdx.x == 0) p.units[a] = total;
+    const int u0 = (int)((int64_t)total * share / p.shares), u1 = (int)((int64_t)total * (share + 1) / p.shares);
+    if (p.shares > 1 && u0 >= u1) return;
+    Mask m;
+    if (q.dropped) m = open_mask(p.drop);
+    f32x4_t acc[RB][8];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    // rows [row, row + have), have <= 32: lane's rows 8 g + j
+    auto unit = [&](int row, int have) __attribute__((always_inline)) {
+        const __amdgpu_buffer_rsrc_t rr = make_rsrc(static_cast<const uint16_t*>(q.r) + (int64_t)row * q.ldr, ((int64_t)(have - 1) * q.ldr + q.cols) * 2);
+        u32x4_t rows[8], r[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) rows[j] = buf_load16(rr, in ? (uint32_t)(((8 * g + j) * q.ldr + n) * 2) : OOB_OFFSET);
+        float v[RB][8];
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+        for (int z = 0; z < q.splits; ++z) {
+            const __amdgpu_buffer_rsrc_t rl = make_rsrc(q.l + z * q.plane + (int64_t)row * p.rank, (int64_t)have * p.rank * 4);
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int k = rank0 + 16 * i + c;
+                    v[i][j] += __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rl, k < p.rank ? ((8 * g + j) * p.rank + k) * 4 : (int)OOB_OFFSET, 0, 0));
+                }
+        }
+        if (q.dropped) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                rows[j] = clear_dropped(m, draw(m, p.drop.group0 + (uint32_t)(n >> 3), p.drop.row0 + (uint32_t)(row + 8 * g + j)), rows[j]);
+        }
+        transpose8(rows, r);
+#pragma unroll
+        for (int i = 0; i < RB; ++i) {
+            u32x4_t term[3];
+            split_terms(v[i], term);
+#pragma unroll
+            for (int s = 0; s < 3; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[i][j] = mfma(term[s], r[j], acc[i][j]);      // rank 16 i + 4 g + e, column 8 c + j
+        }
+    };
+    int base = 0;
+    for (int first = 0; first < p.seg.n && base < u1; first += 64) {
+        int lo, len;
+        segment(p.seg, first + l, lo, len);
+        const int count = len > 0 && adapter(p.seg, first + l) == a ? (len + 31) / 32 : 0, sums = wave_sums(count, l);
+        for (uint64_t some = __ballot(count > 0); some; some &= some - 1) {
+            const int j = __builtin_ctzll(some);
+            const int units = __builtin_amdgcn_readlane(count, j), before = base + __builtin_amdgcn_readlane(sums, j) - units;
+            const int at = __builtin_amdgcn_readlane(lo, j), rows = __builtin_amdgcn_readlane(len, j);
+            int u = before > u0 ? before : u0;
+            u += (w - u) & (GRAD_WAVES - 1);                             // this wave's first one
+            const int end = before + units < u1 ? before + units : u1;
+            for (; u < end; u += GRAD_WAVES) {
+                const int r = 32 * (u - before);
+                unit(at + r, rows - r < 32 ? rows - r : 32);
+            }
+        }
+        base += __builtin_amdgcn_readlane(sums, 63);
+    }
+    const float scale = (p.scale ? p.scale[a] : 1.0f) * (q.dropped ? p.drop.factor : 1.0f);
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+        if (i) __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            *reinterpret_cast<f32x4_t*>(&part[w][4 * g + e][8 * c]) = f32x4_t{acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+            *reinterpret_cast<f32x4_t*>(&part[w][4 * g + e][8 * c + 4]) = f32x4_t{acc[i][4][e], acc[i][5][e], acc[i][6][e], acc[i][7][e]};
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = threadIdx.x + 256 * h, row = at >> 5, col = (at & 31) * 4;
+            const int k = rank0 + 16 * i + row, cc = strip * 128 + col;
+            if (k >= p.rank || cc >= q.cols) continue;
+            f32x4_t s = *reinterpret_cast<const f32x4_t*>(&part[0][row][col]);
+#pragma unroll
+            for (int v = 1; v < GRAD_WAVES; ++v) s += *reinterpret_cast<const f32x4_t*>(&part[v][row][col]);
+            s *= scale;
+            if (p.shares > 1) {
+                *reinterpret_cast<f32x4_t*>(q.part + (((int64_t)a * p.shares + share) * p.rank + k) * q.cols + cc) = s;
+            } else {
+                f32x4_t* const to = reinterpret_cast<f32x4_t*>(q.out + a * q.stride + k * q.ldo + cc);
+                if (p.accumulate) s = *to + s;
+                *to = s;
+            }
+        }
+    }
+}
+// the shares' planes added in order; a share without rows has none
+__global__ __launch_bounds__(256) void tp_adapter_grad_finish_kernel(const GradArgs p) {
+    const int which = blockIdx.y >= (unsigned)p.seg.pool, a = which ? blockIdx.y - p.seg.pool : blockIdx.y;
+    const GradSide& q = p.side[which];
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= (int64_t)p.rank * q.cols) return;
+    const int k = (int)(at / q.cols), cc = (int)(at - (int64_t)k * q.cols);
+    const int64_t total = p.units[a];
+    f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int z = 0; z < p.shares; ++z)
+        if (total * z / p.shares < total * (z + 1) / p.shares)
+            s += *reinterpret_cast<const f32x4_t*>(q.part + ((int64_t)a * p.shares + z) * p.rank * q.cols + at);
+    f32x4_t* const to = reinterpret_cast<f32x4_t*>(q.out + a * q.stride + k * q.ldo + cc);
+    if (p.accumulate) s = *to + s;
+    *to = s;
+}
+
+template <int MT, int RB>
+hipError_t down(const DownArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)a.tiles, (unsigned)a.splits);
+    return launch_kernel(a.dropped ? tp_adapter_down_kernel<MT, RB, true> : tp_adapter_down_kernel<MT, RB, false>, grid, dim3(64 * DOWN_WAVES), 0, s, a);
+}
+template <int MT>
+hipError_t down_rank(const DownArgs& a, hipStream_t s) {
+    return a.rank <= 16 ? down<MT, 1>(a, s) : a.rank <= 32 ? down<MT, 2>(a, s) : a.rank <= 64 ? down<MT, 4>(a, s) : down<MT, 8>(a, s);
+}
+
+template <int GP>
+hipError_t up(const UpArgs& a, hipStream_t s) {
+    const int strips = (a.cols + 127) / 128;
+    const int waves = (int64_t)a.tiles * ((strips + 3) / 4) < 256 ? 1 : 4;      // few rows: a workgroup a strip
+    const dim3 grid((unsigned)a.tiles, (unsigned)((strips + waves - 1) / waves)), block(64 * waves);
+    return launch_kernel(a.out_f32 ? (a.dropped ? tp_adapter_up_kernel<GP, 3, true> : tp_adapter_up_kernel<GP, 3, false>)
+                                   : (a.dropped ? tp_adapter_up_kernel<GP, 2, true> : tp_adapter_up_kernel<GP, 2, false>), grid, block, 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_down(const DownArgs& a, hipStream_t s) {
+    if (a.tiles < 1) return hipSuccess;
+    switch (a.tile) {
+        case 16: return down_rank<1>(a, s);
+        case 64: return down_rank<4>(a, s);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+hipError_t launch_up(const UpArgs& a, hipStream_t s) {
+    if (a.tiles < 1) return hipSuccess;
+    return a.rank <= 16 ? up<2>(a, s) : a.rank <= 32 ? up<4>(a, s) : a.rank <= 64 ? up<8>(a, s) : up<16>(a, s);
+}
+
+hipError_t launch_grad(const GradArgs& a, hipStream_t s) {
+    const int strips0 = (a.side[0].cols + 127) / 128, strips = strips0 + (a.sides > 1 ? (a.side[1].cols + 127) / 128 : 0);
+    const int rb = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4, chunks = (a.rank + 16 * rb - 1) / (16 * rb);
+    const int64_t blocks = (int64_t)strips * chunks * a.shares * a.seg.pool;
+    if (blocks > INT32_MAX || a.seg.pool > 32767) return hipErrorInvalidValue;
+    if (hipError_t e = launch_kernel(rb == 1 ? tp_adapter_grad_kernel<1> : rb == 2 ? tp_adapter_grad_kernel<2> : tp_adapter_grad_kernel<4>,
+                                     dim3((unsigned)blocks), dim3(64 * GRAD_WAVES), 0, s, a, strips0, strips); e != hipSuccess || a.shares == 1)
+        return e;
+    int64_t most = 0;
+    for (int i = 0; i < a.sides; ++i) most = a.side[i].cols > most ? a.side[i].cols : most;
+    const int64_t x = (most * a.rank / 4 + 255) / 256;
+    return launch_kernel(tp_adapter_grad_finish_kernel, dim3((unsigned)x, (unsigned)(a.seg.pool * a.sides)), dim3(256), 0, s, a);
+}
+
+}  // namespace tpl

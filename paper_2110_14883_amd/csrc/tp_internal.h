@@ -80,6 +80,58 @@ hipError_t launch_dropout(const DropArgs& drop, const void* x, int64_t ldx, int 
 hipError_t launch_dropout_bwd(const DropArgs& drop, const void* dy, int64_t ld_dy, const void* pre, int64_t ld_pre, void* dx, int64_t ld_dx, int64_t rows,
                               int64_t cols, float* db, float* ws, hipStream_t stream);     // db (ws: colsum_ws_bytes or null) may be null
 
+// Low-rank adapters (tp_adapters_t, tp_adapter.hip).  Which rows use which adapter, as the kernels take it
+struct SegArgs {
+    const int32_t *offsets, *ids;
+    int32_t n, rows, pool;               // segments, rows of the block, adapters
+};
+// V = P F^T for every row's own factor: P blocks [rows, K] and factors [pool][rank, K] of n_steps steps, summed
+struct DownArgs {
+    const void *p[TP_MAX_STEPS], *f[TP_MAX_STEPS];
+    int64_t strides[TP_MAX_STEPS];       // elements from one adapter's factor to the next one's
+    int32_t ldp[TP_MAX_STEPS], ldf[TP_MAX_STEPS];
+    uint32_t group0[TP_MAX_STEPS];       // of the dropout mask: first group of eight columns of the step's P block
+    int32_t n_steps, K, rank;
+    int32_t tile, tiles, splits;         // rows of a tile, upper bound of the tiles, workgroups sharing K
+    SegArgs seg;
+    int32_t dropped;
+    DropArgs drop;
+    float* out; int64_t plane;           // [splits][rows][rank]
+};
+hipError_t launch_down(const DownArgs& args, hipStream_t stream);
+// out = act(c + bias + s drop(V F)) for every row's own factor F: [rank, cols] and scale s
+struct UpArgs {
+    const float* v; int64_t plane; int32_t splits;     // V as launch_down leaves it
+    float* v_out;                        // the planes' sum, or null
+    const void* f; int64_t stride; int32_t ldf, rank, cols;
+    const float* scale;
+    const void* c; int64_t ldc; int32_t c_f32;
+    const void* bias; int32_t gelu;
+    void* out; int64_t ldo; int32_t out_f32;
+    void* pre; int64_t ldp;
+    int32_t tile, tiles;
+    SegArgs seg;
+    int32_t dropped;
+    DropArgs drop;
+};
+hipError_t launch_up(const UpArgs& args, hipStream_t stream);
+// G_i = s_i L^T drop(R) over the rows of adapter i, for one or two pairs (L: fp32 [rows, rank], R: [rows, cols])
+struct GradSide {
+    const float* l; int64_t plane; int32_t splits;
+    const void* r; int32_t ldr, cols, dropped;
+    float* out; int64_t ldo, stride;     // [pool][rank, cols]
+    float* part;                         // [pool][shares][rank][cols] of shares > 1
+};
+struct GradArgs {
+    GradSide side[2];
+    int32_t sides, rank, shares, accumulate;
+    const float* scale;
+    SegArgs seg;
+    DropArgs drop;
+    int32_t* units;                      // [pool] of shares > 1
+};
+hipError_t launch_grad(const GradArgs& args, hipStream_t stream);
+
 // tile ids: macro-tile shapes the GEMM kernel is instantiated for
 enum TileId { TILE_256x256 = 1, TILE_128x256 = 2, TILE_256x128 = 3, TILE_128x128 = 4,
               TILE_256x256_W4 = 5,     // 256 x 256 by the four-wave stream kernel (tp_gemm4.hip)

@@ -1,5 +1,7 @@
-// C ABI of what stands beside the layer's products (see include/tp_linear.h): dropout without a stored mask.  Everything is checked before the
+// C ABI of what stands beside the layer's products (see include/tp_linear.h): dropout without a stored mask, low-rank
+// adapters.  Everything is checked before the
 // first launch; nothing is allocated or synchronised here.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -26,9 +28,218 @@ int check_dropout(const tp_dropout_t* d, int64_t row, int64_t col, int64_t rows,
     return TP_OK;
 }
 
+// ---------------------------------------------------------------------------------------------
+// adapters
+// ---------------------------------------------------------------------------------------------
+struct Map {            // one pass of tp_block_map
+    int n_steps, a_row[TP_MAX_STEPS], a_col[TP_MAX_STEPS], out_row, out_col, partial;
+    int64_t m, n, k;
+};
+int block_map(const tp_grid_t* grid, const tp_dims_t* dims, int pass, Map* s) {
+    if (int e = tp_block_map(grid, dims, pass, &s->n_steps, &s->m, &s->n, &s->k, s->a_row, s->a_col, nullptr, nullptr, &s->out_row, &s->out_col, &s->partial))
+        return e;
+    return s->m > INT32_MAX || s->n > INT32_MAX || s->k > INT32_MAX ? TP_ERR_SHAPE : TP_OK;
+}
+
+int check_counts(const tp_adapters_t* a) {
+    if (!a) return TP_ERR_NULL;
+    if (a->n_segments < 0 || a->n_adapters < 1 || a->n_adapters > TP_ADAPTER_MAX_POOL || a->rank < 1 || a->rank > TP_ADAPTER_MAX_RANK) return TP_ERR_SHAPE;
+    return a->rank & 7 ? TP_ERR_ALIGN : TP_OK;
+}
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+int check_adapters(const tp_adapters_t* a) {
+    if (int e = check_counts(a)) return e;
+    if (a->n_segments > 0 && (!a->offsets || !a->ids)) return TP_ERR_NULL;
+    return aligned4(a->offsets) && aligned4(a->ids) && aligned4(a->scale) ? TP_OK : TP_ERR_ALIGN;
+}
+int check_factor(const void* ptr, int64_t ld, int64_t stride, const tp_adapters_t* a, int64_t cols) {
+    if (int e = check_cblk(tp_cblk_t{ptr, ld}, cols)) return e;
+    if (stride & 7) return TP_ERR_ALIGN;
+    return a->n_adapters > 1 && stride < (int64_t)(a->rank - 1) * ld + cols ? TP_ERR_SHAPE : TP_OK;
+}
+// an operand and the output over it: the same block or apart
+int check_over(const tp_oblk_t& c, const tp_oblk_t& y, int64_t rows, int64_t cols) {
+    if (c.ptr == y.ptr && c.ld == y.ld && c.dtype == y.dtype) return TP_OK;
+    auto bytes = [&](const tp_oblk_t& b) { return span(b.ptr, b.ld, rows, cols, b.dtype == TP_F32 ? 4 : 2); };
+    return overlap(bytes(c), bytes(y)) ? TP_ERR_SHAPE : TP_OK;
+}
+
+// Tiles of at most `tile` rows that segments over `rows` rows can have
+int64_t most_tiles(int64_t rows, int64_t segments, int tile) {
+    const int64_t some = std::min(rows, segments);        // segments with rows
+    return (rows + some * (tile - 1)) / tile;
+}
+// How the products run.  Short segments (up to 24 rows on average) take tiles of 16 rows, others of 64.  K is shared by as many workgroups of eight
+// waves as make two for every CU, while a wave keeps a unit of 64.
+struct Split { int tile, splits; int64_t tiles; };
+Split plan_down(int64_t rows, int64_t segments, int64_t k, int n_steps) {
+    Split s;
+    s.tile = rows <= 24 * std::max<int64_t>(1, std::min(rows, segments)) ? 16 : 64;
+    s.tiles = std::max<int64_t>(1, most_tiles(rows, segments, s.tile));
+    const int64_t units = (k + 63) / 64 * n_steps;
+    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / s.tiles, units / 8, 16}));
+    return s;
+}
+// Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) for four a CU, 128 rows a share at least
+int plan_grad(int64_t rows, int64_t cols, int pool, int rank) {
+    const int64_t blocks = (cols + 127) / 128 * ((rank + 63) / 64) * pool;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(1024 + blocks - 1) / blocks, rows / 128, 32}));
+}
+size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+// the workspace, in this order
+struct Space { size_t low, da, db, units; size_t all() const { return padded(low) + padded(da) + padded(db) + padded(units); } };
+Space space_fwd(const Map& f, const tp_adapters_t* a) {
+    const Split s = plan_down(f.m, a->n_segments, f.k, f.n_steps);
+    return Space{(size_t)s.splits * (size_t)f.m * a->rank * 4, 0, 0, 0};
+}
+Space space_bwd(const Map& f, const Map& x, const tp_adapters_t* a) {
+    const Split s = plan_down(x.m, a->n_segments, x.k, x.n_steps);
+    const size_t shares = (size_t)plan_grad(x.m, x.n + f.n, a->n_adapters, a->rank), each = shares * a->n_adapters * a->rank * 4;
+    Space w{(size_t)s.splits * (size_t)x.m * a->rank * 4, 0, 0, 0};
+    if (shares > 1) { w.da = each * x.n; w.db = each * f.n; w.units = (size_t)a->n_adapters * 4; }
+    return w;
+}
+
+SegArgs segments(const tp_adapters_t* a, int64_t rows) { return SegArgs{a->offsets, a->ids, a->n_segments, (int32_t)rows, a->n_adapters}; }
+
+// V = sum P_k F_k^T; n_steps blocks, the plan's planes at `planes`
+int fill_down(DownArgs& d, const Split& s, const tp_adapters_t* a, int n_steps, const tp_cblk_t* p, const tp_factor_t* f, int64_t rows, int64_t k, float* planes) {
+    for (int i = 0; i < n_steps; ++i) {
+        if (int e = check_cblk(p[i], k)) return e;
+        if (int e = check_factor(f[i].ptr, f[i].ld, f[i].stride, a, k)) return e;
+        d.p[i] = p[i].ptr; d.ldp[i] = (int32_t)p[i].ld;
+        d.f[i] = f[i].ptr; d.ldf[i] = (int32_t)f[i].ld; d.strides[i] = f[i].stride;
+    }
+    d.n_steps = n_steps; d.K = (int32_t)k; d.rank = a->rank;
+    d.tile = s.tile; d.tiles = (int32_t)s.tiles; d.splits = s.splits;
+    d.seg = segments(a, rows);
+    d.out = planes; d.plane = rows * a->rank;
+    return TP_OK;
+}
+int fill_up(UpArgs& u, const Split& s, const tp_adapters_t* a, const tp_factor_t& f, const tp_oblk_t& c, const tp_oblk_t& out, int64_t rows, int64_t cols) {
+    if (int e = check_factor(f.ptr, f.ld, f.stride, a, cols)) return e;
+    if (int e = check_oblk(c, cols, false)) return e;
+    if (int e = check_oblk(out, cols, false)) return e;
+    if (int e = check_over(c, out, rows, cols)) return e;
+    u.plane = rows * a->rank; u.splits = s.splits;
+    u.f = f.ptr; u.ldf = (int32_t)f.ld; u.stride = f.stride; u.rank = a->rank; u.cols = (int32_t)cols;
+    u.scale = a->scale;
+    u.c = c.ptr; u.ldc = c.ld; u.c_f32 = c.dtype == TP_F32;
+    u.out = out.ptr; u.ldo = out.ld; u.out_f32 = out.dtype == TP_F32;
+    u.tile = s.tile; u.tiles = (int32_t)s.tiles;
+    u.seg = segments(a, rows);
+    return TP_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t tp_adapter_workspace_size(const tp_grid_t* grid, const tp_dims_t* dims, int pass, const tp_adapters_t* adapters) {
+    Map f, x;
+    if (check_counts(adapters) != TP_OK || block_map(grid, dims, TP_PASS_FWD, &f) != TP_OK || block_map(grid, dims, TP_PASS_DX, &x) != TP_OK) return 0;
+    return pass == TP_PASS_FWD ? space_fwd(f, adapters).all() : pass == TP_PASS_DX ? space_bwd(f, x, adapters).all() : 0;
+}
+
+int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, const tp_adapters_t* adapters, const tp_cblk_t* x_blocks,
+                   const tp_factor_t* a_blocks, const tp_factor_t* b, const tp_dropout_t* drop, tp_oblk_t c, const void* bias, int epi, tp_oblk_t y,
+                   tp_oblk_t preact, float* v, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    Map s;
+    if (int e = block_map(grid, dims, TP_PASS_FWD, &s)) return e;
+    if (int e = check_adapters(adapters)) return e;
+    if (!x_blocks || !a_blocks || !b) return TP_ERR_NULL;
+    if (n_steps < 1 || n_steps > s.n_steps) return TP_ERR_SHAPE;
+    if (epi != TP_EPI_NONE && epi != TP_EPI_BIAS && epi != TP_EPI_BIAS_GELU) return TP_ERR_MODE;
+    if (epi != TP_EPI_NONE && !bias) return TP_ERR_NULL;
+    if ((bias && !aligned16(bias)) || !aligned16(v)) return TP_ERR_ALIGN;
+    if (s.partial) {
+        if (epi != TP_EPI_NONE || preact.ptr) return TP_ERR_MODE;
+        if (y.ptr && y.dtype != TP_F32) return TP_ERR_DTYPE;
+    }
+    const Split sp = plan_down(s.m, adapters->n_segments, s.k, s.n_steps);
+    const Space need = space_fwd(s, adapters);
+    float* const planes = v && sp.splits == 1 ? v : static_cast<float*>(workspace);
+    DownArgs d{};
+    if (int e = fill_down(d, sp, adapters, n_steps, x_blocks, a_blocks, s.m, s.k, planes)) return e;
+    if (drop) {
+        d.dropped = 1;
+        for (int i = 0; i < n_steps; ++i) {
+            if (int e = check_dropout(drop, s.a_row[i] * s.m, s.a_col[i] * s.k, s.m, s.k, &d.drop)) return e;
+            d.group0[i] = d.drop.group0;
+        }
+    }
+    UpArgs u{};
+    if (int e = fill_up(u, sp, adapters, *b, c, y, s.m, s.n)) return e;
+    if (preact.ptr) {
+        if (int e = check_oblk(preact, s.n, false)) return e;
+        if (preact.dtype != TP_BF16) return TP_ERR_DTYPE;
+    }
+    u.v = planes; u.v_out = planes == v ? nullptr : v;
+    u.bias = epi == TP_EPI_NONE ? nullptr : bias; u.gelu = epi == TP_EPI_BIAS_GELU;
+    u.pre = preact.ptr; u.ldp = preact.ld;
+    if (!ws_ok(need.all(), workspace, workspace_bytes)) return TP_ERR_WORKSPACE;
+    if (adapters->n_segments == 0) return TP_OK;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    return launch_down(d, stream) != hipSuccess || launch_up(u, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
+}
+
+int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, const tp_adapters_t* adapters, const tp_cblk_t* dy_blocks,
+                   const tp_factor_t* b_blocks, const tp_factor_t* a, const tp_dropout_t* drop, tp_oblk_t dx_base, tp_oblk_t dx, const tp_cblk_t* x_own,
+                   tp_factor_out_t da, const tp_cblk_t* dy_own, const float* v, tp_factor_out_t db, int accumulate, void* workspace,
+                   size_t workspace_bytes, void* hip_stream) {
+    Map f, x;
+    if (int e = block_map(grid, dims, TP_PASS_FWD, &f)) return e;
+    if (int e = block_map(grid, dims, TP_PASS_DX, &x)) return e;
+    if (int e = check_adapters(adapters)) return e;
+    const bool want_u = dx.ptr || da.ptr;
+    if (want_u && (!dy_blocks || !b_blocks)) return TP_ERR_NULL;
+    if (want_u && (n_steps < 1 || n_steps > x.n_steps)) return TP_ERR_SHAPE;
+    if ((dx.ptr && !a) || (da.ptr && !x_own) || (db.ptr && (!dy_own || !v))) return TP_ERR_NULL;
+    if (!aligned16(v)) return TP_ERR_ALIGN;
+    if (dx.ptr && x.partial && dx.dtype != TP_F32) return TP_ERR_DTYPE;
+    const Split sp = plan_down(x.m, adapters->n_segments, x.k, x.n_steps);
+    const Space need = space_bwd(f, x, adapters);
+    char* at = static_cast<char*>(workspace);
+    float* const planes = reinterpret_cast<float*>(at);
+    DropArgs mask{};
+    if (drop)                                         // (rows and columns of the own X block, which dX has too)
+        if (int e = check_dropout(drop, x.out_row * x.m, x.out_col * x.n, x.m, x.n, &mask)) return e;
+    DownArgs d{};
+    if (want_u)
+        if (int e = fill_down(d, sp, adapters, n_steps, dy_blocks, b_blocks, x.m, x.k, planes)) return e;
+    UpArgs u{};
+    if (dx.ptr) {
+        if (int e = fill_up(u, sp, adapters, *a, dx_base, dx, x.m, x.n)) return e;
+        u.v = planes;
+        u.dropped = drop != nullptr; u.drop = mask;
+    }
+    GradArgs g{};
+    auto side = [&](const float* l, int splits, const tp_cblk_t& r, int64_t cols, int dropped, const tp_factor_out_t& out, size_t part) {
+        if (int e = check_cblk(r, cols)) return e;
+        if (int e = check_factor(out.ptr, out.ld, out.stride, adapters, cols)) return e;
+        GradSide& q = g.side[g.sides++];
+        q.l = l; q.plane = x.m * adapters->rank; q.splits = splits;
+        q.r = r.ptr; q.ldr = (int32_t)r.ld; q.cols = (int32_t)cols; q.dropped = dropped;
+        q.out = static_cast<float*>(out.ptr); q.ldo = out.ld; q.stride = out.stride;
+        q.part = reinterpret_cast<float*>(at + part);
+        return (int)TP_OK;
+    };
+    if (da.ptr)
+        if (int e = side(planes, sp.splits, *x_own, x.n, drop != nullptr, da, padded(need.low))) return e;
+    if (db.ptr)
+        if (int e = side(v, 1, *dy_own, f.n, 0, db, padded(need.low) + padded(need.da))) return e;
+    g.rank = adapters->rank; g.shares = plan_grad(x.m, x.n + f.n, adapters->n_adapters, adapters->rank); g.accumulate = accumulate != 0;
+    g.scale = adapters->scale; g.seg = segments(adapters, x.m); g.drop = mask;
+    g.units = reinterpret_cast<int32_t*>(at + padded(need.low) + padded(need.da) + padded(need.db));
+    if (!want_u && !db.ptr) return TP_OK;
+    if (!ws_ok(need.all(), workspace, workspace_bytes)) return TP_ERR_WORKSPACE;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (adapters->n_segments > 0) {
+        if (want_u && launch_down(d, stream) != hipSuccess) return TP_ERR_HIP;
+        if (dx.ptr && launch_up(u, stream) != hipSuccess) return TP_ERR_HIP;
+    }
+    return g.sides && launch_grad(g, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
+}
 
 int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_dtype, const void* bias, int epi, tp_cblk_t residual, tp_oblk_t y,
                    tp_oblk_t preact, int64_t rows, int64_t cols, void* hip_stream) {

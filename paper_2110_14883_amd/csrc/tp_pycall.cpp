@@ -17,8 +17,8 @@
 namespace {
 
 PyObject *s_data_ptr, *s_stride, *s_shape, *s_dtype, *s_numel, *s_element_size;      // interned names
-PyObject *s_get_device;
-PyObject *g_f32, *g_bf16;                                                            // torch.float32, torch.bfloat16
+PyObject *s_get_device, *s_is_contiguous;
+PyObject *g_i32, *g_f32, *g_bf16;                                                            // torch.int32, torch.float32, torch.bfloat16
 PyObject *g_current_device;                                                          // callable, or None: its answer is not compared
 
 decltype(&tp_linear_fwd_ex) f_fwd;
@@ -30,6 +30,8 @@ decltype(&tp_dgelu) f_dgelu;
 decltype(&tp_bias_grad) f_bias_grad;
 decltype(&tp_dropout_fwd) f_dropout_fwd;
 decltype(&tp_dropout_bwd) f_dropout_bwd;
+decltype(&tp_adapter_fwd) f_adapter_fwd;
+decltype(&tp_adapter_bwd) f_adapter_bwd;
 
 // Every helper returns false with a Python exception set.
 struct Ref {                                       // an owned reference
@@ -367,6 +369,142 @@ PyObject* dropout_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return f_dropout_bwd(&d, dy.ptr, dy.ld, pre.ptr, pre.ld, const_cast<void*>(dx.ptr), dx.ld, db, rows, cols, ws.ptr, ws.bytes, stream);
     });
 }
+// A call's adapters: a sequence (offsets, ids, n_adapters, rank, scale, n_segments); n_segments None: as many as ids has
+bool numel(PyObject* o, int64_t* n) { return call0(o, s_numel, n); }
+bool to_adapters(PyObject* o, tp_adapters_t* a, Devices* at) {
+    Ref s(PySequence_Fast(o, "adapters must be an Adapters"));
+    if (!s) return false;
+    if (PySequence_Fast_GET_SIZE(s.p) != 6) {
+        PyErr_SetString(PyExc_ValueError, "adapters must be an Adapters: (offsets, ids, n_adapters, rank, scale, n_segments)");
+        return false;
+    }
+    PyObject** it = PySequence_Fast_ITEMS(s.p);
+    void *offsets, *ids, *scale;
+    int pool, rank;
+    int64_t n = 0;
+    if (!look(it[0], g_i32, at) || !look(it[1], g_i32, at) || !look(it[4], g_f32, at) || !to_ptr(it[0], &offsets) || !to_ptr(it[1], &ids) ||
+        !to_int(it[2], &pool) || !to_int(it[3], &rank) || !to_ptr(it[4], &scale) || (it[5] != Py_None && !to_i64(it[5], &n)))
+        return false;
+    auto flat = [&](PyObject* t, int64_t want, const char* what) {        // a tensor of at least that many elements, one behind the other
+        if (t == Py_None || PyLong_Check(t)) return true;
+        int64_t have;
+        if (!numel(t, &have)) return false;
+        Ref c(PyObject_CallMethodNoArgs(t, s_is_contiguous));
+        if (!c) return false;
+        if (have >= want && c.p == Py_True) return true;
+        PyErr_Format(PyExc_ValueError, "%s must be a contiguous tensor of %lld elements", what, (long long)want);
+        return false;
+    };
+    if (it[5] == Py_None && it[1] != Py_None && !PyLong_Check(it[1]) && !numel(it[1], &n)) return false;
+    if (n < 0 || n > INT32_MAX - 1) n = -1;                              // (the library answers)
+    if (!flat(it[0], n > 0 ? n + 1 : 0, "offsets") || !flat(it[1], n > 0 ? n : 0, "ids") || !flat(it[4], pool, "scale")) return false;
+    *a = tp_adapters_t{static_cast<const int32_t*>(offsets), static_cast<const int32_t*>(ids), static_cast<const float*>(scale), (int32_t)n, pool, rank};
+    return true;
+}
+// A factor: a tensor [n_adapters, rank, cols] with unit column stride, (address, leading dimension, stride) or None
+template <class F> bool to_factor(PyObject* o, F* f, const tp_adapters_t& a, PyObject* type, Devices* at) {
+    int64_t ptr = 0, ld = 0, stride = 0;
+    if (o != Py_None) {
+        bool tensor;
+        if (!is_tensor(o, &tensor)) return false;
+        if (!tensor) {
+            if (!item(o, 0, &ptr) || !item(o, 1, &ld) || !item(o, 2, &stride)) return false;
+        } else {
+            if (!look(o, type, at) || !call0(o, s_data_ptr, &ptr)) return false;
+            Ref st(PyObject_CallMethodNoArgs(o, s_stride)), sh(PyObject_GetAttr(o, s_shape));
+            if (!st || !sh) return false;
+            int64_t n, r, unit;
+            if (PySequence_Size(st.p) != 3 || !item(sh.p, 0, &n) || !item(sh.p, 1, &r) || !item(st.p, 0, &stride) || !item(st.p, 1, &ld) || !item(st.p, 2, &unit)) {
+                if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a factor must be [n_adapters, rank, cols]");
+                return false;
+            }
+            if (n != a.n_adapters || r != a.rank || unit != 1) {
+                PyErr_SetString(PyExc_ValueError, "a factor must be [n_adapters, rank, cols] with unit column stride");
+                return false;
+            }
+            if (n == 1) stride = 0;                                      // (never used; torch puts anything there)
+        }
+    }
+    f->ptr = reinterpret_cast<decltype(f->ptr)>(ptr);
+    f->ld = ld;
+    f->stride = stride;
+    return true;
+}
+struct Factors {
+    tp_factor_t at_[TP_MAX_STEPS] = {};
+    const tp_factor_t* ptr = nullptr;
+    bool fill(PyObject* o, const tp_adapters_t& a, Devices* at) {
+        if (o == Py_None) return true;
+        if (PyObject_Size(o) < 0) return false;
+        Ref s(PySequence_Fast(o, "factors must be a sequence"));
+        if (!s) return false;
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(s.p);
+        if (n > TP_MAX_STEPS) { PyErr_SetString(PyExc_ValueError, "too many factors"); return false; }
+        for (Py_ssize_t i = 0; i < n; ++i)
+            if (!to_factor(PySequence_Fast_GET_ITEM(s.p, i), at_ + i, a, g_bf16, at)) return false;
+        ptr = at_;
+        return true;
+    }
+};
+bool look_all(PyObject* o, PyObject* want, Devices* at) {
+    if (o == Py_None || PyObject_Size(o) < 0) return !PyErr_Occurred();
+    Ref s(PySequence_Fast(o, "blocks must be a sequence"));
+    if (!s) return false;
+    for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(s.p); ++i)
+        if (!look(PySequence_Fast_GET_ITEM(s.p, i), want, at)) return false;
+    return true;
+}
+// V: fp32 [rows, rank], one row behind the other
+bool to_v(PyObject* o, float** v, Devices* at) {
+    void* p;
+    if (!look(o, g_f32, at) || !to_ptr(o, &p)) return false;
+    if (o != Py_None && !PyLong_Check(o)) {
+        Ref c(PyObject_CallMethodNoArgs(o, s_is_contiguous));
+        if (!c) return false;
+        if (c.p != Py_True) { PyErr_SetString(PyExc_ValueError, "v must be contiguous"); return false; }
+    }
+    *v = static_cast<float*>(p);
+    return true;
+}
+struct MaybeDropout {
+    tp_dropout_t d;
+    const tp_dropout_t* ptr = nullptr;
+    bool fill(PyObject* o, Devices* at) {
+        if (o == Py_None) return true;
+        if (!to_dropout(o, &d, at)) return false;
+        ptr = &d;
+        return true;
+    }
+};
+// adapter_fwd(grid, dims, n_steps, adapters, x_blocks, a_blocks, b, dropout, c, bias, epi, y, preact, v, workspace, stream)
+PyObject* adapter_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    const tp_grid_t* grid; tp_dims_t dims; int steps, epi; tp_adapters_t ad; CBlocks x; Factors f; tp_factor_t b; MaybeDropout drop; tp_oblk_t c, y, pre;
+    void *bias, *stream; float* v; Workspace ws; Devices at;
+    if (!count(n, 16) || !to_struct(a[0], &grid) || !to_dims(a[1], &dims) || !to_int(a[2], &steps) || !to_adapters(a[3], &ad, &at) ||
+        !look_all(a[4], g_bf16, &at) || !x.fill(a[4]) || !f.fill(a[5], ad, &at) || !to_factor(a[6], &b, ad, g_bf16, &at) || !drop.fill(a[7], &at) ||
+        !look(a[8], nullptr, &at) || !to_oblk(a[8], &c) || !look(a[9], g_bf16, &at) || !to_ptr(a[9], &bias) || !to_int(a[10], &epi) ||
+        !look(a[11], nullptr, &at) || !to_oblk(a[11], &y) || !look(a[12], nullptr, &at) || !to_oblk(a[12], &pre) || !to_v(a[13], &v, &at) ||
+        !look(a[14], nullptr, &at) || !to_ws(a[14], &ws) || !to_ptr(a[15], &stream))
+        return nullptr;
+    return answer([&] {
+        return f_adapter_fwd(grid, &dims, steps, &ad, x.ptr, f.ptr, a[6] == Py_None ? nullptr : &b, drop.ptr, c, bias, epi, y, pre, v, ws.ptr, ws.bytes, stream);
+    });
+}
+// adapter_bwd(grid, dims, n_steps, adapters, dy_blocks, b_blocks, a, dropout, dx_base, dx, x_own, da, dy_own, v, db, accumulate, workspace, stream)
+PyObject* adapter_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    const tp_grid_t* grid; tp_dims_t dims; int steps, accumulate; tp_adapters_t ad; CBlocks dy; Factors f; tp_factor_t fa; MaybeDropout drop;
+    tp_oblk_t base, dx; MaybeBlock x, own; tp_factor_out_t da, db; float* v; void* stream; Workspace ws; Devices at;
+    if (!count(n, 18) || !to_struct(a[0], &grid) || !to_dims(a[1], &dims) || !to_int(a[2], &steps) || !to_adapters(a[3], &ad, &at) ||
+        !look_all(a[4], g_bf16, &at) || !dy.fill(a[4]) || !f.fill(a[5], ad, &at) || !to_factor(a[6], &fa, ad, g_bf16, &at) || !drop.fill(a[7], &at) ||
+        !look(a[8], nullptr, &at) || !to_oblk(a[8], &base) || !look(a[9], nullptr, &at) || !to_oblk(a[9], &dx) || !look(a[10], g_bf16, &at) || !x.fill(a[10]) ||
+        !to_factor(a[11], &da, ad, g_f32, &at) || !look(a[12], g_bf16, &at) || !own.fill(a[12]) || !to_v(a[13], &v, &at) ||
+        !to_factor(a[14], &db, ad, g_f32, &at) || !to_int(a[15], &accumulate) || !look(a[16], nullptr, &at) || !to_ws(a[16], &ws) || !to_ptr(a[17], &stream))
+        return nullptr;
+    return answer([&] {
+        return f_adapter_bwd(grid, &dims, steps, &ad, dy.ptr, f.ptr, a[6] == Py_None ? nullptr : &fa, drop.ptr, base, dx, x.ptr, da, own.ptr, v, db, accumulate,
+                             ws.ptr, ws.bytes, stream);
+    });
+}
 // bind(addresses of the first seven functions in the order above, torch.float32, torch.bfloat16)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* f[7];
@@ -385,13 +523,16 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-// bind_ops(addresses of the functions behind those, a function that gives the current device or None)
+// bind_ops(addresses of the functions behind those, torch.int32, a function that gives the current device or None)
 PyObject* bind_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    void* f[2];
-    if (!count(n, 3)) return nullptr;
-    for (int i = 0; i < 2; ++i)
+    void* f[4];
+    if (!count(n, 6)) return nullptr;
+    for (int i = 0; i < 4; ++i)
         if (!to_ptr(a[i], &f[i])) return nullptr;
-    Py_INCREF(a[2]); Py_XSETREF(g_current_device, a[2]);
+    Py_INCREF(a[4]); Py_XSETREF(g_i32, a[4]);
+    Py_INCREF(a[5]); Py_XSETREF(g_current_device, a[5]);
+    f_adapter_fwd = reinterpret_cast<decltype(f_adapter_fwd)>(f[2]);
+    f_adapter_bwd = reinterpret_cast<decltype(f_adapter_bwd)>(f[3]);
     f_dropout_fwd = reinterpret_cast<decltype(f_dropout_fwd)>(f[0]);
     f_dropout_bwd = reinterpret_cast<decltype(f_dropout_bwd)>(f[1]);
     Py_RETURN_NONE;
@@ -400,14 +541,15 @@ PyObject* bind_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
 PyMethodDef methods[] = {{"fwd", FAST(fwd)}, {"fwd_static", FAST(fwd_static)}, {"bwd", FAST(bwd)}, {"bwd_partials", FAST(bwd_partials)},
                          {"bias_act", FAST(bias_act)}, {"dgelu", FAST(dgelu)}, {"bias_grad", FAST(bias_grad)}, {"bind", FAST(bind)},
-                         {"dropout_fwd", FAST(dropout_fwd)}, {"dropout_bwd", FAST(dropout_bwd)}, {"bind_ops", FAST(bind_ops)},
+                         {"dropout_fwd", FAST(dropout_fwd)}, {"dropout_bwd", FAST(dropout_bwd)}, {"adapter_fwd", FAST(adapter_fwd)},
+                         {"adapter_bwd", FAST(adapter_bwd)}, {"bind_ops", FAST(bind_ops)},
                          {nullptr, nullptr, 0, nullptr}};
 // (Set up in its exec slot: a second load of the file makes a module of its own.  A module set up in one go would fill the one that stands under
 // this name in sys.modules, which may be another copy's.)
 int exec(PyObject*) {
     struct { PyObject** to; const char* name; } names[] = {{&s_data_ptr, "data_ptr"}, {&s_stride, "stride"}, {&s_shape, "shape"},
                                                            {&s_dtype, "dtype"}, {&s_numel, "numel"}, {&s_element_size, "element_size"},
-                                                           {&s_get_device, "get_device"}};
+                                                           {&s_get_device, "get_device"}, {&s_is_contiguous, "is_contiguous"}};
     for (auto& x : names)
         if (!*x.to && !(*x.to = PyUnicode_InternFromString(x.name))) return -1;
     return 0;
