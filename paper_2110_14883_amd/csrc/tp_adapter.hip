@@ -31,20 +31,19 @@ __device__ __forceinline__ int wave_sums(int x, int l) {
     }
     return x;
 }
-// rows [lo, lo + len) of segment i, clamped
-__device__ __forceinline__ void segment(const SegArgs& s, int i, int& lo, int& len) {
+// rows [lo, lo + len) of segment i, clamped, and its adapter (-1: none)
+__device__ __forceinline__ void segment(const SegArgs& s, int i, int& lo, int& len, int& id) {
     lo = len = 0;
+    id = -1;
     if (i < s.n) {
         lo = s.offsets[i];
         int hi = s.offsets[i + 1];
+        const int k = s.ids[i];
         lo = lo < 0 ? 0 : lo > s.rows ? s.rows : lo;
         hi = hi < 0 ? 0 : hi > s.rows ? s.rows : hi;
         len = hi > lo ? hi - lo : 0;
+        id = k >= 0 && k < s.pool ? k : -1;
     }
-}
-__device__ __forceinline__ int adapter(const SegArgs& s, int i) {      // -1: none
-    const int id = s.ids[i];
-    return id >= 0 && id < s.pool ? id : -1;
 }
 
 struct Tile { int row0, rows, id; };
@@ -53,8 +52,8 @@ __device__ __forceinline__ bool find_tile(const SegArgs& s, int t, int T, Tile& 
     const int l = threadIdx.x & 63;
     int base = 0;
     for (int first = 0; first < s.n; first += 64) {
-        int lo, len;
-        segment(s, first + l, lo, len);
+        int lo, len, id;
+        segment(s, first + l, lo, len, id);
         const int count = (len + T - 1) / T, sums = wave_sums(count, l);
         const uint64_t behind = __ballot(base + sums > t);
         if (behind) {
@@ -62,7 +61,7 @@ __device__ __forceinline__ bool find_tile(const SegArgs& s, int t, int T, Tile& 
             const int at = __builtin_amdgcn_readlane(lo, j), end = at + __builtin_amdgcn_readlane(len, j);
             out.row0 = at + (t - base - (__builtin_amdgcn_readlane(sums, j) - __builtin_amdgcn_readlane(count, j))) * T;
             out.rows = end - out.row0 < T ? end - out.row0 : T;
-            out.id = uni(adapter(s, first + j));
+            out.id = __builtin_amdgcn_readlane(id, j);
             return out.row0 >= at && out.rows > 0;               // (not so only where sums of wild offsets overflow)
         }
         base += __builtin_amdgcn_readlane(sums, 63);
@@ -183,144 +182,190 @@ __global__ __launch_bounds__(64 * DOWN_WAVES) void tp_adapter_down_kernel(const 
 }
 
 // ---------------------------------------------------------------------------------------------
-// up.  A wave has a strip of 128 columns of a tile's rows: it turns the strip of its adapter's factor into matrix operands once, eight 16-column
-// blocks whose columns are 8 c + j, so that a lane ends up with eight neighbouring columns of four rows: whole 16-byte pieces of C and Y,
-// and one draw a row.
-// GP: groups of eight ranks (2: up to 16 ranks, where both halves of the wave's k range hold the same ranks and the terms of V lie
-// side by side in it; 4, 8, 16: up to 32, 64, 128 ranks).
+// up.  A workgroup has a tile of rows and, a wave each, strips of 128 columns.  It first lays V's terms out in LDS, as the rows of the second product's
+// left operand: first terms, second terms (third ones) of a row's ranks one behind the other, so that for up to 16 ranks two terms fill one matrix
+// instruction's 32 k.  A wave turns its strip of the factor into matrix operands once, eight 16-column blocks, so that a lane ends up with eight
+// columns of four rows: columns 8 c .. 8 c + 7 where C and the result are bf16, else 4 c .. 4 c + 3 and 64 + 4 c .. + 3, which makes every access of
+// a row 16 (8) neighbouring bytes a lane and one draw a row either way.  (32 bytes a lane in two halves: each streamed store is half of a sector.)
+// The next 16 rows of C are on their way while these are finished.
+// GP: groups of eight ranks (2, 4, 8, 16: up to 16, 32, 64, 128 ranks; those beyond the rank are zeros).
 // ---------------------------------------------------------------------------------------------
-template <int GP, int TERMS, bool DROP>
-__global__ __launch_bounds__(256) void tp_adapter_up_kernel(const UpArgs p) {
-    constexpr int NS = GP >= 4 ? GP / 4 : 1;
+template <int GP, int TERMS> struct UpShape {
+    static constexpr int NS = GP >= 4 ? GP / 4 : 1;                      // blocks of 32 k that the factor has
+    static constexpr int STEPS = (TERMS * GP + 3) / 4;                   // and V's terms
+    static constexpr int ROW = STEPS * 64 + 16;                          // bytes of a row in LDS (16 more: rows start in different banks)
+    template <bool C32> static constexpr bool AHEAD = GP < 16 || !C32;   // whether there are registers for the next rows of C
+};
+template <bool C32> struct CRows { u32x4_t v[4][C32 ? 2 : 1]; };
+template <int GP, int TERMS, bool DROP, bool C32>
+__global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
+    using Sh = UpShape<GP, TERMS>;
+    constexpr bool AHEAD = Sh::template AHEAD<C32>;
+    constexpr bool O32 = TERMS == 3, WIDE = !C32 && !O32;
+    extern __shared__ __attribute__((aligned(16))) char low[];
     const int l = threadIdx.x & 63, c = l & 15, g = l >> 4;
     const int strip = uni(blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6));
-    if (strip * 128 >= p.cols) return;
     Tile t;
     if (!find_tile(p.seg, blockIdx.x, p.tile, t)) return;
-    const int n = strip * 128 + 8 * c;
-    const bool in = n < p.cols;
-    auto group = [&](int s) __attribute__((always_inline)) { return GP >= 4 ? 4 * s + g : g & (GP - 1); };
-    u32x4_t f[NS][8];
-    float scale = 1.0f;
-    if (t.id >= 0) {
-        if (p.scale) scale = p.scale[t.id];
-        const __amdgpu_buffer_rsrc_t rf = make_rsrc(static_cast<const uint16_t*>(p.f) + t.id * p.stride, ((int64_t)(p.rank - 1) * p.ldf + p.cols) * 2);
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            u32x4_t rows[8];
-            const bool ok = in && 8 * group(s) < p.rank;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) rows[j] = buf_load16(rf, ok ? (uint32_t)(((8 * group(s) + j) * p.ldf + n) * 2) : OOB_OFFSET);
-            transpose8(rows, f[s]);
-        }
-    }
-    Mask m;
-    if constexpr (DROP) m = open_mask(p.drop);
-    float b[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (p.bias && in) {
-        const u32x4_t q = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(p.bias) + n);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { b[2 * i] = bf16_lo(q[i]); b[2 * i + 1] = bf16_hi(q[i]); }
-    }
-    for (int r0 = 0; r0 < t.rows; r0 += 16) {
-        // C of rows r0 + 4 g + e (past the end: the last row; past the columns: the first ones)
-        u32x4_t cv[4][2];
+    const bool adapted = t.id >= 0;
+    // the lane's columns: n .. n + 7, or n .. n + 3 and n + 64 .. n + 67
+    const int n = strip * 128 + (WIDE ? 8 : 4) * c;
+    const bool in = n < p.cols, in1 = WIDE ? in : n + 64 < p.cols;
+    // C of rows r0 + 4 g + e (past the end: the last row; past the columns: the first ones)
+    constexpr int CB = C32 ? 4 : 2;
+    const char* const c0 = static_cast<const char*>(p.c) + (int64_t)t.row0 * p.ldc * CB;
+    const int at0 = (in ? n : 0) * CB, at1 = (in1 ? n + 64 : 0) * CB;
+    auto load_c = [&](CRows<C32>& q, int r0) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int r = r0 + 4 * g + e < t.rows ? r0 + 4 * g + e : t.rows - 1;
-            const int64_t at = (int64_t)(t.row0 + r) * p.ldc + (in ? n : 0);
-            if (p.c_f32) {
-                const u32x4_t* const src = reinterpret_cast<const u32x4_t*>(static_cast<const float*>(p.c) + at);
-                cv[e][0] = __builtin_nontemporal_load(src);
-                cv[e][1] = __builtin_nontemporal_load(src + 1);
+            const char* const row = c0 + r * p.ldc * CB;
+            if constexpr (C32) {
+                q.v[e][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row + at0));
+                q.v[e][1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row + at1));
+            } else if constexpr (WIDE) {
+                q.v[e][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row + at0));
             } else {
-                cv[e][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(p.c) + at));
-                cv[e][1] = cv[e][0];
+                const u32x2_t a = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(row + at0));
+                const u32x2_t b = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(row + at1));
+                q.v[e][0] = u32x4_t{a[0], a[1], b[0], b[1]};
             }
+        }
+    };
+    // eight bf16 values of a row at `base` (16 bytes, or 8 and 8), and back
+    auto load_row = [&](const __amdgpu_buffer_rsrc_t& rs, int k, bool ok) __attribute__((always_inline)) {
+        const uint32_t at = (uint32_t)((k * p.ldf + n) * 2);
+        if constexpr (WIDE) return buf_load16(rs, ok && in ? at : OOB_OFFSET);
+        const u32x2_t a = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(ok && in ? at : OOB_OFFSET), 0, 0);
+        const u32x2_t b = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(ok && in1 ? at + 128 : OOB_OFFSET), 0, 0);
+        return u32x4_t{a[0], a[1], b[0], b[1]};
+    };
+    auto store_bf16 = [&](void* base, int64_t ld, int64_t row, const float (&v)[8]) __attribute__((always_inline)) {
+        uint16_t* const to = static_cast<uint16_t*>(base) + row * ld + n;
+        const u32x4_t o = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        if constexpr (WIDE) {
+            if (in) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t*>(to));
+        } else {
+            if (in) __builtin_nontemporal_store(u32x2_t{o[0], o[1]}, reinterpret_cast<u32x2_t*>(to));
+            if (in1) __builtin_nontemporal_store(u32x2_t{o[2], o[3]}, reinterpret_cast<u32x2_t*>(to + 64));
+        }
+    };
+    u32x4_t f[Sh::NS][8];
+    CRows<C32> next;
+    if (adapted) {
+        const __amdgpu_buffer_rsrc_t rf = make_rsrc(static_cast<const uint16_t*>(p.f) + t.id * p.stride, ((int64_t)(p.rank - 1) * p.ldf + p.cols) * 2);
+#pragma unroll
+        for (int s = 0; s < Sh::NS; ++s) {
+            const int k = 8 * (GP >= 4 ? 4 * s + g : g & (GP - 1));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[s][j] = load_row(rf, k + j, k < p.rank);
+        }
+        if constexpr (AHEAD) load_c(next, 0);
+        // V's terms; eight ranks of a row a thread
+        const float scale = (p.scale ? p.scale[t.id] : 1.0f) * (DROP ? p.drop.factor : 1.0f);
+        for (int i = threadIdx.x; i < t.rows * GP; i += blockDim.x) {
+            const int r = i / GP, q = i % GP;
+            float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (8 * q < p.rank) {
+                const int64_t at = (int64_t)(t.row0 + r) * p.rank + 8 * q;
+                for (int z = 0; z < p.splits; ++z) {
+                    const f32x4_t *src = reinterpret_cast<const f32x4_t*>(p.v + z * p.plane + at), a = src[0], b = src[1];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) { v[k] += a[k]; v[4 + k] += b[k]; }
+                }
+                if (p.v_out && blockIdx.y == 0) {
+                    f32x4_t* const to = reinterpret_cast<f32x4_t*>(p.v_out + at);
+                    to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+                    to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] *= scale;
+            }
+            u32x4_t term[TERMS];
+            split_terms(v, term);
+#pragma unroll
+            for (int s = 0; s < TERMS; ++s) *reinterpret_cast<u32x4_t*>(low + r * Sh::ROW + (s * GP + q) * 16) = term[s];
+            if constexpr (Sh::STEPS * 4 > TERMS * GP) *reinterpret_cast<u32x4_t*>(low + r * Sh::ROW + (TERMS * GP + q) * 16) = u32x4_t{0u, 0u, 0u, 0u};
+        }
+#pragma unroll
+        for (int s = 0; s < Sh::NS; ++s) {
+            u32x4_t o[8];
+            transpose8(f[s], o);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[s][j] = o[j];
+        }
+    } else if constexpr (AHEAD) {
+        load_c(next, 0);
+    }
+    __syncthreads();
+    if (strip * 128 >= p.cols) return;
+    Mask m;
+    if constexpr (DROP) m = open_mask(p.drop);
+    u32x4_t bias = {0u, 0u, 0u, 0u};
+    if (p.bias) {
+        const char* const b = static_cast<const char*>(p.bias);
+        if constexpr (WIDE) {
+            bias = *reinterpret_cast<const u32x4_t*>(b + (in ? n : 0) * 2);
+        } else {
+            const u32x2_t q = *reinterpret_cast<const u32x2_t*>(b + (in ? n : 0) * 2), s = *reinterpret_cast<const u32x2_t*>(b + (in1 ? n + 64 : 0) * 2);
+            bias = u32x4_t{q[0], q[1], s[0], s[1]};
+        }
+    }
+    for (int r0 = 0; r0 < t.rows; r0 += 16) {
+        CRows<C32> cv;
+        if constexpr (AHEAD) {
+            cv = next;
+            if (r0 + 16 < t.rows) load_c(next, r0 + 16);
+        } else {
+            load_c(cv, r0);
         }
         f32x4_t acc[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        if (t.id >= 0) {
+        if (adapted) {
+            const int r = r0 + c < t.rows ? r0 + c : t.rows - 1;
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (r0 + c < t.rows && 8 * group(s) < p.rank) {
-                    const int64_t at = (int64_t)(t.row0 + r0 + c) * p.rank + 8 * group(s);
-                    for (int z = 0; z < p.splits; ++z) {
-                        const f32x4_t *src = reinterpret_cast<const f32x4_t*>(p.v + z * p.plane + at), lo = src[0], hi = src[1];
+            for (int s = 0; s < Sh::STEPS; ++s) {
+                const u32x4_t v = *reinterpret_cast<const u32x4_t*>(low + r * Sh::ROW + s * 64 + g * 16);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) { v[i] += lo[i]; v[4 + i] += hi[i]; }
-                    }
-                    if (p.v_out && strip == 0 && (GP >= 4 || g < GP)) {
-                        f32x4_t* const to = reinterpret_cast<f32x4_t*>(p.v_out + at);
-                        to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
-                        to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= scale;
-                u32x4_t term[TERMS];
-                split_terms(v, term);
-                if constexpr (GP >= 4) {
-#pragma unroll
-                    for (int q = 0; q < TERMS; ++q)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) acc[j] = mfma(term[q], f[s][j], acc[j]);
-                } else {
-                    const bool second = g >= 2;
-                    u32x4_t both;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) both[i] = second ? term[1][i] : term[0][i];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[j] = mfma(both, f[s][j], acc[j]);
-                    if constexpr (TERMS == 3) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) both[i] = second ? 0u : term[2][i];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) acc[j] = mfma(both, f[s][j], acc[j]);
-                    }
-                }
+                for (int j = 0; j < 8; ++j) acc[j] = mfma(v, f[s % Sh::NS][j], acc[j]);
             }
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int r = r0 + 4 * g + e;
             float v[8];
-            if (p.c_f32) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = as_float(cv[e][j >> 2][j & 3]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = j & 1 ? bf16_hi(cv[e][0][j >> 1]) : bf16_lo(cv[e][0][j >> 1]);
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (C32) v[j] = as_float(cv.v[e][j >> 2][j & 3]);
+                else               v[j] = j & 1 ? bf16_hi(cv.v[e][0][j >> 1]) : bf16_lo(cv.v[e][0][j >> 1]);
             }
             if constexpr (DROP) {
-                const u32x4_t bits = draw(m, p.drop.group0 + (uint32_t)(n >> 3), p.drop.row0 + (uint32_t)(t.row0 + r));
+                const uint32_t row = p.drop.row0 + (uint32_t)(t.row0 + r), group = p.drop.group0 + (uint32_t)(n >> 3);
+                const u32x4_t bits = WIDE ? draw(m, group, row) : draw_shared(m, group, group + 8, row);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += keeps(m, bits, j) ? acc[j][e] * p.drop.factor : 0.0f;
+                for (int j = 0; j < 8; ++j) v[j] += keeps(m, bits, j) ? acc[j][e] : 0.0f;
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] += acc[j][e];
             }
+            if (p.bias) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += b[j];
-            if (r >= t.rows || !in) continue;
-            const int64_t row = t.row0 + r;
-            if (p.pre) {
-                const u32x4_t s = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-                __builtin_nontemporal_store(s, reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(p.pre) + row * p.ldp + n));
+                for (int j = 0; j < 8; ++j) v[j] += j & 1 ? bf16_hi(bias[j >> 1]) : bf16_lo(bias[j >> 1]);
             }
+            if (r >= t.rows) continue;
+            const int64_t row = t.row0 + r;
+            if (p.pre) store_bf16(p.pre, p.ldp, row, v);
             if (p.gelu) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = gelu_f(v[j]);
             }
-            if (p.out_f32) {
-                f32x4_t* const to = reinterpret_cast<f32x4_t*>(static_cast<float*>(p.out) + row * p.ldo + n);
-                __builtin_nontemporal_store(f32x4_t{v[0], v[1], v[2], v[3]}, to);
-                __builtin_nontemporal_store(f32x4_t{v[4], v[5], v[6], v[7]}, to + 1);
+            if constexpr (O32) {
+                float* const to = static_cast<float*>(p.out) + row * p.ldo + n;
+                if (in) __builtin_nontemporal_store(f32x4_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_t*>(to));
+                if (in1) __builtin_nontemporal_store(f32x4_t{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4_t*>(to + 64));
             } else {
-                const u32x4_t o = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-                __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(p.out) + row * p.ldo + n));
+                store_bf16(p.out, p.ldo, row, v);
             }
         }
     }
@@ -348,9 +393,9 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
     // units of this adapter, those of this share
     int total = 0;
     for (int first = 0; first < p.seg.n; first += 64) {
-        int lo, len;
-        segment(p.seg, first + l, lo, len);
-        const int count = len > 0 && adapter(p.seg, first + l) == a ? (len + 31) / 32 : 0;
+        int lo, len, id;
+        segment(p.seg, first + l, lo, len, id);
+        const int count = id == a ? (len + 31) / 32 : 0;
         total += __builtin_amdgcn_readlane(wave_sums(count, l), 63);
     }
     if (p.shares > 1 && share == 0 && strip_all == 0 && rank0 == 0 && threadIdx.x == 0) p.units[a] = total;
@@ -402,9 +447,9 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
     };
     int base = 0;
     for (int first = 0; first < p.seg.n && base < u1; first += 64) {
-        int lo, len;
-        segment(p.seg, first + l, lo, len);
-        const int count = len > 0 && adapter(p.seg, first + l) == a ? (len + 31) / 32 : 0, sums = wave_sums(count, l);
+        int lo, len, id;
+        segment(p.seg, first + l, lo, len, id);
+        const int count = id == a ? (len + 31) / 32 : 0, sums = wave_sums(count, l);
         for (uint64_t some = __ballot(count > 0); some; some &= some - 1) {
             const int j = __builtin_ctzll(some);
             const int units = __builtin_amdgcn_readlane(count, j), before = base + __builtin_amdgcn_readlane(sums, j) - units;
@@ -475,14 +520,25 @@ hipError_t down_rank(const DownArgs& a, hipStream_t s) {
     return a.rank <= 16 ? down<MT, 1>(a, s) : a.rank <= 32 ? down<MT, 2>(a, s) : a.rank <= 64 ? down<MT, 4>(a, s) : down<MT, 8>(a, s);
 }
 
-template <int GP>
-hipError_t up(const UpArgs& a, hipStream_t s) {
-    const int strips = (a.cols + 127) / 128;
-    const int waves = (int64_t)a.tiles * ((strips + 3) / 4) < 256 ? 1 : 4;      // few rows: a workgroup a strip
-    const dim3 grid((unsigned)a.tiles, (unsigned)((strips + waves - 1) / waves)), block(64 * waves);
-    return launch_kernel(a.out_f32 ? (a.dropped ? tp_adapter_up_kernel<GP, 3, true> : tp_adapter_up_kernel<GP, 3, false>)
-                                   : (a.dropped ? tp_adapter_up_kernel<GP, 2, true> : tp_adapter_up_kernel<GP, 2, false>), grid, block, 0, s, a);
+// Waves of a workgroup of `up`: as few idle ones as possible where the strips are shared out, about four; with few tiles a strip a workgroup
+int up_waves(int strips, int64_t tiles) {
+    if (tiles * ((strips + 3) / 4) < 256) return 1;
+    int best = 4;
+    auto left = [&](int w) { return (strips + w - 1) / w * w - strips; };
+    for (int w : {5, 3, 6})
+        if (left(w) < left(best)) best = w;
+    return best;
 }
+template <int GP, int TERMS>
+hipError_t up_as(const UpArgs& a, hipStream_t s) {
+    const int strips = (a.cols + 127) / 128, waves = up_waves(strips, a.tiles);
+    const dim3 grid((unsigned)a.tiles, (unsigned)((strips + waves - 1) / waves)), block(64 * waves);
+    const size_t lds = (size_t)a.tile * UpShape<GP, TERMS>::ROW;
+    return launch_kernel(a.c_f32 ? (a.dropped ? tp_adapter_up_kernel<GP, TERMS, true, true> : tp_adapter_up_kernel<GP, TERMS, false, true>)
+                                 : (a.dropped ? tp_adapter_up_kernel<GP, TERMS, true, false> : tp_adapter_up_kernel<GP, TERMS, false, false>), grid, block, lds, s, a);
+}
+template <int GP>
+hipError_t up(const UpArgs& a, hipStream_t s) { return a.out_f32 ? up_as<GP, 3>(a, s) : up_as<GP, 2>(a, s); }
 
 }  // namespace
 

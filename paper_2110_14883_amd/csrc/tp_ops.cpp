@@ -77,7 +77,7 @@ Split plan_down(int64_t rows, int64_t segments, int64_t k, int n_steps) {
     s.tile = rows <= 24 * std::max<int64_t>(1, std::min(rows, segments)) ? 16 : 64;
     s.tiles = std::max<int64_t>(1, most_tiles(rows, segments, s.tile));
     const int64_t units = (k + 63) / 64 * n_steps;
-    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / s.tiles, units / 8, 16}));
+    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / s.tiles, units / 8, 16}));
     return s;
 }
 // Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) for four a CU, 128 rows a share at least

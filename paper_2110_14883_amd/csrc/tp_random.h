@@ -20,20 +20,31 @@ __device__ __forceinline__ Mask open_mask(const DropArgs& d) {
     if (d.offset_dev) off += *d.offset_dev;
     return Mask{d.key0, d.key1, (uint32_t)off, (uint32_t)(off >> 32), d.threshold};
 }
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
 // the 128 bits of column group `group` of row `row`
 __device__ __forceinline__ u32x4_t draw(const Mask& m, uint32_t group, uint32_t row) {
     uint32_t x0 = group, x1 = row, x2 = m.off_lo, x3 = m.off_hi, k0 = m.key0, k1 = m.key1;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
         const uint64_t a = (uint64_t)x0 * 0xD2511F53u, b = (uint64_t)x2 * 0xCD9E8D57u;
-        x0 = (uint32_t)(b >> 32) ^ x1 ^ k0;
+        x0 = xor3((uint32_t)(b >> 32), x1, k0);
         x1 = (uint32_t)b;
-        x2 = (uint32_t)(a >> 32) ^ x3 ^ k1;
+        x2 = xor3((uint32_t)(a >> 32), x3, k1);
         x3 = (uint32_t)a;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
     return u32x4_t{x0, x1, x2, x3};
+}
+// The same for a lane that holds columns 4 i .. 4 i + 3 of two stretches of columns, i = its number, `group0` and `group1` the groups of those (lanes
+// 2 j and 2 j + 1 share both): the even lane draws one, the odd one the other, and they hand each other the half that is its neighbour's.
+// Words 0, 1 are the bits of the first four columns, 2, 3 of the others.
+__device__ __forceinline__ u32x4_t draw_shared(const Mask& m, uint32_t group0, uint32_t group1, uint32_t row) {
+    const bool odd = threadIdx.x & 1;
+    const u32x4_t w = draw(m, odd ? group1 : group0, row);
+    const int a = odd ? w[0] : w[2], b = odd ? w[1] : w[3];
+    const uint32_t x = (uint32_t)__builtin_amdgcn_mov_dpp(a, 0xB1, 0xF, 0xF, true), y = (uint32_t)__builtin_amdgcn_mov_dpp(b, 0xB1, 0xF, 0xF, true);   // lanes 1 0 3 2
+    return u32x4_t{odd ? x : w[0], odd ? y : w[1], odd ? w[2] : x, odd ? w[3] : y};
 }
 __device__ __forceinline__ bool keeps(const Mask& m, const u32x4_t& bits, int e) {
     const uint32_t w = bits[e >> 1];
