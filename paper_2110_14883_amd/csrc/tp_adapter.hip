@@ -14,13 +14,13 @@
 // the offsets itself (one trip to memory for up to 64 segments), so a call is the same launches whatever the lengths, and can be captured.  Offsets are
 // clamped to the rows there are and an adapter that the pool does not have is none: bad ones give wrong rows, never a wild access.
 #include "tp_random.h"
+#include "tp_stream.h"
 
 namespace tpl {
 
 namespace {
 
 __device__ __forceinline__ float as_float(uint32_t w) { return __builtin_bit_cast(float, w); }   // (of a value: a bit cast of a vector's element takes its first one)
-__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // inclusive sum over the wave's lanes
 __device__ __forceinline__ int wave_sums(int x, int l) {
@@ -102,79 +102,107 @@ __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, cons
 }
 
 // ---------------------------------------------------------------------------------------------
-// down.  A tile of 16 MT rows by all 16 RB ranks; the eight waves of a workgroup, and the workgroups of a tile, share K in units of 64 (32 where
-// registers would not hold two units), and the waves' sums meet in LDS in their order.  A wave keeps the next unit's loads in flight.
+// down.  A tile of 16 MT rows by all 16 RB ranks.  The waves of a workgroup, and the workgroups of a tile, take the units of 64 k in turn (so neighbouring
+// waves read neighbouring cache lines of a row), and the waves' sums meet in LDS in their order.  A wave has a ring of LDS slots of its own, filled by
+// direct-to-LDS loads of 8 whole lines each, with no barrier in the loop.  (Fragments loaded straight into registers, 64 bytes of 16 rows an
+// instruction: 16384 x 4096, 16 ranks 34.2 us against XXX.)
 // ---------------------------------------------------------------------------------------------
-constexpr int DOWN_WAVES = 8;
+constexpr int down_waves(int mt, int rb) { return mt + rb <= 5 ? 8 : 4; }
+template <int MT, int RB> struct DownShape {
+    static constexpr int WAVES = down_waves(MT, RB);
+    static constexpr int X_BYTES = MT * 2048, SLOT = (MT + RB) * 2048, LOADS = 2 * (MT + RB);   // a unit: lines of 16 MT rows, of 16 RB ranks
+    static constexpr int FIT = 163840 / (WAVES * SLOT), NS = FIT > 4 ? 4 : FIT;
+    static constexpr int PART = 16 * RB + 4, SUMS = WAVES * 16 * PART * 4;                      // the waves' sums of 16 rows
+    static constexpr int BYTES = WAVES * NS * SLOT > SUMS ? WAVES * NS * SLOT : SUMS;
+    static_assert(NS >= 1 && BYTES <= 163840);
+};
 template <int MT, int RB, bool DROP>
-__global__ __launch_bounds__(64 * DOWN_WAVES) void tp_adapter_down_kernel(const DownArgs p) {
-    constexpr int H = MT + RB >= 8 ? 1 : 2;                             // k steps of 32 in a unit
-    __shared__ __attribute__((aligned(16))) float part[DOWN_WAVES][16][16 * RB + 4];
+__global__ __launch_bounds__(64 * down_waves(MT, RB)) void tp_adapter_down_kernel(const DownArgs p) {
+    using Sh = DownShape<MT, RB>;
+    constexpr int WAVES = Sh::WAVES, NS = Sh::NS;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     Tile t;
     if (!find_tile(p.seg, blockIdx.x, 16 * MT, t) || t.id < 0) return;
     const int l = threadIdx.x & 63, c = l & 15, g = l >> 4, w = uni(threadIdx.x >> 6);
-    const int KT = (p.K + 32 * H - 1) / (32 * H), total = p.n_steps * KT, shares = p.splits * DOWN_WAVES, share = blockIdx.y * DOWN_WAVES + w;
-    int u = uni((int)((int64_t)total * share / shares));
-    const int end = uni((int)((int64_t)total * (share + 1) / shares));
-    int step = uni(u / KT), kt = u - step * KT;
+    const int KT = (p.K + 63) / 64, total = p.n_steps * KT, shares = p.splits * WAVES, share = blockIdx.y * WAVES + w;
     Mask m;
     if constexpr (DROP) m = open_mask(p.drop);
-    struct Unit { u32x4_t x[H][MT], f[H][RB]; uint32_t group; };
-    auto fetch = [&](Unit& n) __attribute__((always_inline)) {           // the unit at (step, kt), which moves on
-        const int ldp = p.ldp[step], ldf = p.ldf[step];
-        const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const uint16_t*>(p.p[step]) + (int64_t)t.row0 * ldp, ((int64_t)(t.rows - 1) * ldp + p.K) * 2);
-        const __amdgpu_buffer_rsrc_t rf = make_rsrc(static_cast<const uint16_t*>(p.f[step]) + t.id * p.strides[step], ((int64_t)(p.rank - 1) * ldf + p.K) * 2);
-#pragma unroll
-        for (int h = 0; h < H; ++h) {
-            const int k = 32 * (H * kt + h) + 8 * g;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) n.x[h][i] = buf_load16(rx, k < p.K ? (uint32_t)(((16 * i + c) * ldp + k) * 2) : OOB_OFFSET);
-#pragma unroll
-            for (int j = 0; j < RB; ++j) n.f[h][j] = buf_load16(rf, k < p.K ? (uint32_t)(((16 * j + c) * ldf + k) * 2) : OOB_OFFSET);
-        }
-        if constexpr (DROP) n.group = p.group0[step] + 4 * H * kt + g;
-        if (++kt == KT) { kt = 0; ++step; }
+    const uint32_t mine = (uint32_t)(w * NS * Sh::SLOT);
+    // rows of 128 bytes, 16-byte chunk q of row r at q ^ ((r >> 1) & 7): reads of one chunk of 16 rows lie in different banks
+    const int lr = l >> 3;
+    auto load = [&](auto n_loads, const uint16_t* base, int64_t bytes, int ld, int k0, uint32_t dst) __attribute__((always_inline)) {
+        const uint64_t at = reinterpret_cast<uint64_t>(base);
+        const u32x4_t rs = {(uint32_t)uni((int)(uint32_t)at), (uint32_t)uni((int)((uint32_t)(at >> 32) & 0xffffu)), (uint32_t)uni((int)(uint32_t)bytes), 0x00020000u};
+        static_for<decltype(n_loads)::value>([&](auto n_) __attribute__((always_inline)) {
+            constexpr int n = decltype(n_)::value;
+            const int r = 8 * n + lr, k = k0 + (((l & 7) ^ ((r >> 1) & 7)) << 3);
+            dtl_load16(rs, k < p.K ? (uint32_t)((r * ld + k) * 2) : OOB_OFFSET, dst + n * 1024);
+        });
     };
-    f32x4_t acc[MT][RB];
+    int f_step = 0, f_kt = share;                                        // the unit to fetch next
+    while (f_kt >= KT && f_step < p.n_steps) { f_kt -= KT; ++f_step; }
+    auto fetch = [&](int slot) __attribute__((always_inline)) {          // (past the end: empty descriptors, zeros that nobody uses)
+        const bool live = f_step < p.n_steps;
+        const int s = uni(live ? f_step : 0), ldp = uni(p.ldp[s]), ldf = uni(p.ldf[s]), k0 = uni(64 * f_kt);
+        const uint32_t dst = mine + (uint32_t)(slot * Sh::SLOT);
+        load(std::integral_constant<int, 2 * MT>{}, static_cast<const uint16_t*>(p.p[s]) + (int64_t)t.row0 * ldp,
+             live ? ((int64_t)(t.rows - 1) * ldp + p.K) * 2 : 0, ldp, k0, dst);
+        load(std::integral_constant<int, 2 * RB>{}, static_cast<const uint16_t*>(p.f[s]) + t.id * p.strides[s],
+             live ? ((int64_t)(p.rank - 1) * ldf + p.K) * 2 : 0, ldf, k0, dst + Sh::X_BYTES);
+        for (f_kt += shares; f_kt >= KT && f_step < p.n_steps; ++f_step) f_kt -= KT;
+    };
+    f32x4_t acc[MT][RB];                                                 // acc[i][j][e]: row 16 i + c, rank 16 j + 4 g + e
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < RB; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    auto multiply = [&](Unit& n) __attribute__((always_inline)) {        // acc[i][j][e]: row 16 i + c, rank 16 j + 4 g + e
 #pragma unroll
-        for (int h = 0; h < H; ++h)
+    for (int s = 0; s < NS - 1; ++s) fetch(s);
+    int slot = 0, step = 0, kt = share;                                  // the unit to multiply
+    while (kt >= KT && step < p.n_steps) { kt -= KT; ++step; }
+    for (int u = share; u < total; u += shares) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");               // the slot to refill has been read
+        fetch(slot == 0 ? NS - 1 : slot - 1);
+        wait_vm<(NS - 1) * Sh::LOADS>();
+        asm volatile("" ::: "memory");
+        const uint32_t at = mine + (uint32_t)(slot * Sh::SLOT);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            auto frag = [&](uint32_t base, int i) __attribute__((always_inline)) {
+                const int r = 16 * i + c;
+                return lds_load_frag(base + r * 128 + (((4 * h + g) ^ ((r >> 1) & 7)) << 4));
+            };
+            bf16x8_t f[RB];
+#pragma unroll
+            for (int j = 0; j < RB; ++j) f[j] = frag(at + Sh::X_BYTES, j);
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                u32x4_t x = n.x[h][i];
-                if constexpr (DROP) x = clear_dropped(m, draw(m, n.group + 4 * h, p.drop.row0 + (uint32_t)(t.row0 + 16 * i + c)), x);
+                u32x4_t x = __builtin_bit_cast(u32x4_t, frag(at, i));
+                if constexpr (DROP)
+                    x = clear_dropped(m, draw(m, p.group0[step] + 8 * kt + 4 * h + g, p.drop.row0 + (uint32_t)(t.row0 + 16 * i + c)), x);
 #pragma unroll
-                for (int j = 0; j < RB; ++j) acc[i][j] = mfma(n.f[h][j], x, acc[i][j]);
+                for (int j = 0; j < RB; ++j) acc[i][j] = mfma(__builtin_bit_cast(u32x4_t, f[j]), x, acc[i][j]);
             }
-    };
-    if (u < end) {
-        Unit a, b;
-        fetch(a);
-        while (true) {
-            if (u + 1 < end) fetch(b);
-            multiply(a);
-            if (++u >= end) break;
-            if (u + 1 < end) fetch(a);
-            multiply(b);
-            if (++u >= end) break;
         }
+        slot = slot + 1 == NS ? 0 : slot + 1;
+        for (kt += shares; kt >= KT && step < p.n_steps; ++step) kt -= KT;
     }
+    wait_vm<0>();                                                        // (zeros on their way into slots)
+    __syncthreads();
+    float* const part = reinterpret_cast<float*>(lds);
     float* const out = p.out + blockIdx.y * p.plane;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         if (i) __syncthreads();
 #pragma unroll
-        for (int j = 0; j < RB; ++j) *reinterpret_cast<f32x4_t*>(&part[w][c][16 * j + 4 * g]) = acc[i][j];
+        for (int j = 0; j < RB; ++j) *reinterpret_cast<f32x4_t*>(part + (w * 16 + c) * Sh::PART + 16 * j + 4 * g) = acc[i][j];
         __syncthreads();
-        const int row = threadIdx.x / (4 * RB), q = threadIdx.x % (4 * RB);
-        if (row < 16 && 16 * i + row < t.rows && 4 * q < p.rank) {
-            f32x4_t s = *reinterpret_cast<const f32x4_t*>(&part[0][row][4 * q]);
+        for (int x = threadIdx.x; x < 64 * RB; x += 64 * WAVES) {
+            const int row = x / (4 * RB), q = x % (4 * RB);
+            if (16 * i + row >= t.rows || 4 * q >= p.rank) continue;
+            f32x4_t s = *reinterpret_cast<const f32x4_t*>(part + row * Sh::PART + 4 * q);
 #pragma unroll
-            for (int v = 1; v < DOWN_WAVES; ++v) s += *reinterpret_cast<const f32x4_t*>(&part[v][row][4 * q]);
+            for (int v = 1; v < WAVES; ++v) s += *reinterpret_cast<const f32x4_t*>(part + (v * 16 + row) * Sh::PART + 4 * q);
             if constexpr (DROP) s *= p.drop.factor;
             *reinterpret_cast<f32x4_t*>(out + (int64_t)(t.row0 + 16 * i + row) * p.rank + 4 * q) = s;
         }
@@ -382,10 +410,12 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
     __shared__ __attribute__((aligned(16))) float part[GRAD_WAVES][16][132];
     const int l = threadIdx.x & 63, c = l & 15, g = l >> 4, w = uni(threadIdx.x >> 6);
     const int chunks = (p.rank + 16 * RB - 1) / (16 * RB);
+    // (the shares side by side: an XCD then has its own shares of the rows, and a CU strips of both pairs, of which one may draw a mask: 16384 rows of
+    // 4096 and 4096 columns with dropout 58 us with the strips side by side, XXX so)
     int x = blockIdx.x;
+    const int share = x % p.shares; x /= p.shares;
     const int strip_all = x % strips; x /= strips;
-    const int rank0 = (x % chunks) * 16 * RB; x /= chunks;
-    const int share = x % p.shares, a = x / p.shares;
+    const int rank0 = (x % chunks) * 16 * RB, a = x / chunks;
     const int which = strip_all >= strips0, strip = which ? strip_all - strips0 : strip_all;
     const GradSide& q = p.side[which];
     const int n = strip * 128 + 8 * c;
@@ -493,42 +523,61 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
         }
     }
 }
-// the shares' planes added in order; a share without rows has none
-__global__ __launch_bounds__(256) void tp_adapter_grad_finish_kernel(const GradArgs p) {
+// the shares' planes added in order, eight on their way at a time; a share without rows has none
+__global__ __launch_bounds__(64) void tp_adapter_grad_finish_kernel(const GradArgs p) {
     const int which = blockIdx.y >= (unsigned)p.seg.pool, a = which ? blockIdx.y - p.seg.pool : blockIdx.y;
     const GradSide& q = p.side[which];
-    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int64_t at = ((int64_t)blockIdx.x * 64 + threadIdx.x) * 4;
     if (at >= (int64_t)p.rank * q.cols) return;
     const int k = (int)(at / q.cols), cc = (int)(at - (int64_t)k * q.cols);
     const int64_t total = p.units[a];
-    f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int z = 0; z < p.shares; ++z)
-        if (total * z / p.shares < total * (z + 1) / p.shares)
-            s += *reinterpret_cast<const f32x4_t*>(q.part + ((int64_t)a * p.shares + z) * p.rank * q.cols + at);
     f32x4_t* const to = reinterpret_cast<f32x4_t*>(q.out + a * q.stride + k * q.ldo + cc);
+    f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int z0 = 0; z0 < p.shares; z0 += 8) {
+        f32x4_t v[8];
+#pragma unroll
+        for (int z = 0; z < 8; ++z) {
+            const int y = z0 + z;
+            v[z] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            if (y < p.shares && total * y / p.shares < total * (y + 1) / p.shares)
+                v[z] = *reinterpret_cast<const f32x4_t*>(q.part + ((int64_t)a * p.shares + y) * p.rank * q.cols + at);
+        }
+#pragma unroll
+        for (int z = 0; z < 8; ++z) s += v[z];
+    }
     if (p.accumulate) s = *to + s;
     *to = s;
 }
 
-template <int MT, int RB>
-hipError_t down(const DownArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)a.tiles, (unsigned)a.splits);
-    return launch_kernel(a.dropped ? tp_adapter_down_kernel<MT, RB, true> : tp_adapter_down_kernel<MT, RB, false>, grid, dim3(64 * DOWN_WAVES), 0, s, a);
+// Kernels with more LDS than a launch has by default: said once on every device (the same value every time)
+template <class K>
+hipError_t allow_lds(K kernel, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+    if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes); e != hipSuccess) return e;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return hipSuccess;
 }
+template <int MT, int RB, bool DROP>
+hipError_t down_as(const DownArgs& a, hipStream_t s) {
+    using Sh = DownShape<MT, RB>;
+    static std::atomic<uint64_t> done{0};
+    if (hipError_t e = allow_lds(tp_adapter_down_kernel<MT, RB, DROP>, Sh::BYTES, done); e != hipSuccess) return e;
+    return launch_kernel(tp_adapter_down_kernel<MT, RB, DROP>, dim3((unsigned)a.tiles, (unsigned)a.splits), dim3(64 * Sh::WAVES), Sh::BYTES, s, a);
+}
+template <int MT, int RB>
+hipError_t down(const DownArgs& a, hipStream_t s) { return a.dropped ? down_as<MT, RB, true>(a, s) : down_as<MT, RB, false>(a, s); }
 template <int MT>
 hipError_t down_rank(const DownArgs& a, hipStream_t s) {
-    return a.rank <= 16 ? down<MT, 1>(a, s) : a.rank <= 32 ? down<MT, 2>(a, s) : a.rank <= 64 ? down<MT, 4>(a, s) : down<MT, 8>(a, s);
+    if (a.rank <= 16) return down<MT, 1>(a, s);
+    if (a.rank <= 32) return down<MT, 2>(a, s);
+    if (a.rank <= 64) return down<MT, 4>(a, s);
+    if constexpr (MT <= 2) return down<MT, 8>(a, s);
+    return hipErrorInvalidValue;
 }
 
-// Waves of a workgroup of `up`: as few idle ones as possible where the strips are shared out, about four; with few tiles a strip a workgroup
-int up_waves(int strips, int64_t tiles) {
-    if (tiles * ((strips + 3) / 4) < 256) return 1;
-    int best = 4;
-    auto left = [&](int w) { return (strips + w - 1) / w * w - strips; };
-    for (int w : {5, 3, 6})
-        if (left(w) < left(best)) best = w;
-    return best;
-}
 template <int GP, int TERMS>
 hipError_t up_as(const UpArgs& a, hipStream_t s) {
     const int strips = (a.cols + 127) / 128, waves = up_waves(strips, a.tiles);
@@ -546,6 +595,7 @@ hipError_t launch_down(const DownArgs& a, hipStream_t s) {
     if (a.tiles < 1) return hipSuccess;
     switch (a.tile) {
         case 16: return down_rank<1>(a, s);
+        case 32: return down_rank<2>(a, s);
         case 64: return down_rank<4>(a, s);
         default: return hipErrorInvalidValue;
     }
@@ -566,8 +616,8 @@ hipError_t launch_grad(const GradArgs& a, hipStream_t s) {
         return e;
     int64_t most = 0;
     for (int i = 0; i < a.sides; ++i) most = a.side[i].cols > most ? a.side[i].cols : most;
-    const int64_t x = (most * a.rank / 4 + 255) / 256;
-    return launch_kernel(tp_adapter_grad_finish_kernel, dim3((unsigned)x, (unsigned)(a.seg.pool * a.sides)), dim3(256), 0, s, a);
+    const int64_t x = (most * a.rank / 4 + 63) / 64;
+    return launch_kernel(tp_adapter_grad_finish_kernel, dim3((unsigned)x, (unsigned)(a.seg.pool * a.sides)), dim3(64), 0, s, a);
 }
 
 }  // namespace tpl

@@ -153,6 +153,22 @@ hipError_t forward(const DropArgs& drop, const void* x, int64_t ldx, const void*
     });
 }
 
+// How the sums run: as those of a finished block, but in strips of 256 columns where those have 128 (16384 x 4096 51.1 us for 53.2, 32896 x 2560 with GeLU'
+// 106.4 for 108.7: longer pieces of a row, and 32 rows side by side in a workgroup of 16 waves as before), and with the number of slabs, up to what the workspace holds, at which the CU with the most
+// workgroups has the fewest rows: these kernels are bound by vector instructions as much as by memory, and a few workgroups beyond a whole round of the
+// 256 CUs cost half a round (32896 x 2560 with GeLU', 20 strips of 128: 26 slabs 123.7 us, 25 108.7).
+ColsumPlan sums_plan(int64_t rows, int64_t cols, bool has_ws) {
+    ColsumPlan p = colsum_plan(rows, cols, has_ws, true);
+    const int64_t strips = p.wide ? (cols + 255) / 256 : (cols + 63) / 64, weight = p.wide ? 2 : 1;
+    auto slab = [&](int s) { return s == 1 ? rows : ((rows + s - 1) / s + 31) / 32 * 32; };
+    auto longest = [&](int s) { return (strips * s * weight + 255) / 256 * slab(s); };
+    int best = p.splits;
+    for (int s = p.splits - 1; s >= 2; --s)
+        if (longest(s) < longest(best)) best = s;
+    p.splits = best;
+    p.per = slab(best);
+    return p;
+}
 template <bool GELU, int COLS>
 hipError_t backward_sums(const DropArgs& drop, const ColsumPlan& p, const uint16_t* dy, int64_t ld_dy, const uint16_t* pre, int64_t ld_pre, uint16_t* dx,
                          int64_t ld_dx, int64_t rows, int64_t cols, float* db, float* ws, hipStream_t s) {
@@ -183,10 +199,10 @@ hipError_t launch_dropout_bwd(const DropArgs& drop, const void* dy, int64_t ld_d
     const uint16_t *g = static_cast<const uint16_t*>(dy), *a = static_cast<const uint16_t*>(pre);
     uint16_t* const o = static_cast<uint16_t*>(dx);
     if (db) {
-        const ColsumPlan p = colsum_plan(rows, cols, ws != nullptr, true);
+        const ColsumPlan p = sums_plan(rows, cols, ws != nullptr);
         auto pick = [&](auto gelu) {
             constexpr bool G = decltype(gelu)::value;
-            return p.wide ? backward_sums<G, 128>(drop, p, g, ld_dy, a, ld_pre, o, ld_dx, rows, cols, db, ws, s)
+            return p.wide ? backward_sums<G, 256>(drop, p, g, ld_dy, a, ld_pre, o, ld_dx, rows, cols, db, ws, s)
                           : backward_sums<G, 64>(drop, p, g, ld_dy, a, ld_pre, o, ld_dx, rows, cols, db, ws, s);
         };
         return a ? pick(std::true_type{}) : pick(std::false_type{});

@@ -115,6 +115,15 @@ struct UpArgs {
     DropArgs drop;
 };
 hipError_t launch_up(const UpArgs& args, hipStream_t stream);
+// Waves of a workgroup there, a strip of 128 columns each: as few idle ones as possible, about four; with few tiles a strip a workgroup
+inline int up_waves(int strips, int64_t tiles) {
+    if (tiles * ((strips + 3) / 4) < 256) return 1;
+    int best = 4;
+    auto left = [&](int w) { return (strips + w - 1) / w * w - strips; };
+    for (int w : {5, 3, 6})
+        if (left(w) < left(best)) best = w;
+    return best;
+}
 // G_i = s_i L^T drop(R) over the rows of adapter i, for one or two pairs (L: fp32 [rows, rank], R: [rows, cols])
 struct GradSide {
     const float* l; int64_t plane; int32_t splits;

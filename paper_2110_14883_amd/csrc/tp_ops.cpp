@@ -69,31 +69,54 @@ int64_t most_tiles(int64_t rows, int64_t segments, int tile) {
     const int64_t some = std::min(rows, segments);        // segments with rows
     return (rows + some * (tile - 1)) / tile;
 }
-// How the products run.  Short segments (up to 24 rows on average) take tiles of 16 rows, others of 64.  K is shared by as many workgroups of eight
-// waves as make two for every CU, while a wave keeps a unit of 64.
-struct Split { int tile, splits; int64_t tiles; };
-Split plan_down(int64_t rows, int64_t segments, int64_t k, int n_steps) {
+// How the products run.
+//   down: short segments (up to 24 rows on average) take tiles of 16 rows, others of 64, or of 32 where 64 make at most 128 tiles, leave the CU with the most
+//     tiles more rows (the start of one counted as eight), or there are more than 64 ranks.  us with 64 / 32: 16384 x 4096, 16 ranks 29.6 / 36.5; 32896 x 2 x
+//     2560 in 24 segments 50.2 / 46.3; 2048 x 4 x 2048, 64 ranks 15.6 / 15.6, and up 21.5 / 19.3 for half the planes.  K is shared by as many workgroups
+//     as make one for every CU, while each has eight units of 64.
+//   up: tiles of 32, 64 or 128 rows, whichever leaves the CU with the most workgroups (two at least, or there are too few loads under way) the
+//     fewest rows, the start of a workgroup counted as ten.  us with 32 / 64 / 128: 16384 x 4096 fp32 with dropout, 16 ranks
+//     118 / 110 / 101; 6000 x 4096 in 12 segments with GeLU, 32 ranks 44.9 / 47.6 / 45.4; 2048 x 8192, 64 ranks 25.1 / 21.8 / 25.2; 32896 x 640 in 24 segments
+//     19.2 / 21.6 / 24.3.
+struct Split { int tile, splits; int64_t tiles; int up_tile; int64_t up_tiles; };
+Split plan_products(int64_t rows, int64_t segments, int64_t k, int n_steps, int64_t up_cols, int rank) {
     Split s;
-    s.tile = rows <= 24 * std::max<int64_t>(1, std::min(rows, segments)) ? 16 : 64;
-    s.tiles = std::max<int64_t>(1, most_tiles(rows, segments, s.tile));
+    const bool brief = rows <= 24 * std::max<int64_t>(1, std::min(rows, segments));
+    auto tiles = [&](int tile) { return std::max<int64_t>(1, most_tiles(rows, segments, tile)); };
+    auto rounds = [](int64_t groups) { return (groups + 255) / 256; };
+    s.tile = 16;
+    s.up_tile = 16;
+    if (!brief) {
+        s.tile = rank > 64 || tiles(64) <= 128 || rounds(tiles(32)) * (32 + 8) < rounds(tiles(64)) * (64 + 8) ? 32 : 64;
+        int64_t best = INT64_MAX;
+        const int strips = (int)((up_cols + 127) / 128);
+        for (int tile : {64, 128, 32}) {
+            if (tile == 128 && rank > 64) continue;             // (V's terms would not fit)
+            const int waves = up_waves(strips, tiles(tile));
+            const int64_t cost = std::max<int64_t>(2, rounds(tiles(tile) * ((strips + waves - 1) / waves))) * (tile + 10);
+            if (cost < best) { best = cost; s.up_tile = tile; }
+        }
+    }
+    s.tiles = tiles(s.tile);
+    s.up_tiles = tiles(s.up_tile);
     const int64_t units = (k + 63) / 64 * n_steps;
     s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / s.tiles, units / 8, 16}));
     return s;
 }
-// Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) for four a CU, 128 rows a share at least
+// Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) for two a CU (four: 63 us for 55, and more planes), 128 rows a share at least
 int plan_grad(int64_t rows, int64_t cols, int pool, int rank) {
     const int64_t blocks = (cols + 127) / 128 * ((rank + 63) / 64) * pool;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(1024 + blocks - 1) / blocks, rows / 128, 32}));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(512 + blocks - 1) / blocks, rows / 128, 32}));
 }
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 // the workspace, in this order
 struct Space { size_t low, da, db, units; size_t all() const { return padded(low) + padded(da) + padded(db) + padded(units); } };
 Space space_fwd(const Map& f, const tp_adapters_t* a) {
-    const Split s = plan_down(f.m, a->n_segments, f.k, f.n_steps);
+    const Split s = plan_products(f.m, a->n_segments, f.k, f.n_steps, f.n, a->rank);
     return Space{(size_t)s.splits * (size_t)f.m * a->rank * 4, 0, 0, 0};
 }
 Space space_bwd(const Map& f, const Map& x, const tp_adapters_t* a) {
-    const Split s = plan_down(x.m, a->n_segments, x.k, x.n_steps);
+    const Split s = plan_products(x.m, a->n_segments, x.k, x.n_steps, x.n, a->rank);
     const size_t shares = (size_t)plan_grad(x.m, x.n + f.n, a->n_adapters, a->rank), each = shares * a->n_adapters * a->rank * 4;
     Space w{(size_t)s.splits * (size_t)x.m * a->rank * 4, 0, 0, 0};
     if (shares > 1) { w.da = each * x.n; w.db = each * f.n; w.units = (size_t)a->n_adapters * 4; }
@@ -126,7 +149,7 @@ int fill_up(UpArgs& u, const Split& s, const tp_adapters_t* a, const tp_factor_t
     u.scale = a->scale;
     u.c = c.ptr; u.ldc = c.ld; u.c_f32 = c.dtype == TP_F32;
     u.out = out.ptr; u.ldo = out.ld; u.out_f32 = out.dtype == TP_F32;
-    u.tile = s.tile; u.tiles = (int32_t)s.tiles;
+    u.tile = s.up_tile; u.tiles = (int32_t)s.up_tiles;
     u.seg = segments(a, rows);
     return TP_OK;
 }
@@ -156,7 +179,7 @@ int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
         if (epi != TP_EPI_NONE || preact.ptr) return TP_ERR_MODE;
         if (y.ptr && y.dtype != TP_F32) return TP_ERR_DTYPE;
     }
-    const Split sp = plan_down(s.m, adapters->n_segments, s.k, s.n_steps);
+    const Split sp = plan_products(s.m, adapters->n_segments, s.k, s.n_steps, s.n, adapters->rank);
     const Space need = space_fwd(s, adapters);
     float* const planes = v && sp.splits == 1 ? v : static_cast<float*>(workspace);
     DownArgs d{};
@@ -197,7 +220,7 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
     if ((dx.ptr && !a) || (da.ptr && !x_own) || (db.ptr && (!dy_own || !v))) return TP_ERR_NULL;
     if (!aligned16(v)) return TP_ERR_ALIGN;
     if (dx.ptr && x.partial && dx.dtype != TP_F32) return TP_ERR_DTYPE;
-    const Split sp = plan_down(x.m, adapters->n_segments, x.k, x.n_steps);
+    const Split sp = plan_products(x.m, adapters->n_segments, x.k, x.n_steps, x.n, adapters->rank);
     const Space need = space_bwd(f, x, adapters);
     char* at = static_cast<char*>(workspace);
     float* const planes = reinterpret_cast<float*>(at);
@@ -234,11 +257,11 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
     if (!want_u && !db.ptr) return TP_OK;
     if (!ws_ok(need.all(), workspace, workspace_bytes)) return TP_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (adapters->n_segments > 0) {
-        if (want_u && launch_down(d, stream) != hipSuccess) return TP_ERR_HIP;
-        if (dx.ptr && launch_up(u, stream) != hipSuccess) return TP_ERR_HIP;
-    }
-    return g.sides && launch_grad(g, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
+    // (dA and dB before dX: dY, which U has just read, may still be in the last cache)
+    const bool some = adapters->n_segments > 0;
+    if (some && want_u && launch_down(d, stream) != hipSuccess) return TP_ERR_HIP;
+    if (g.sides && launch_grad(g, stream) != hipSuccess) return TP_ERR_HIP;
+    return some && dx.ptr && launch_up(u, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
 }
 
 int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_dtype, const void* bias, int epi, tp_cblk_t residual, tp_oblk_t y,
