@@ -22,13 +22,14 @@ namespace {
 
 __device__ __forceinline__ float as_float(uint32_t w) { return __builtin_bit_cast(float, w); }   // (of a value: a bit cast of a vector's element takes its first one)
 
-// inclusive sum over the wave's lanes
-__device__ __forceinline__ int wave_sums(int x, int l) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int o = __shfl_up(x, d);
-        if (l >= d) x += o;
-    }
+// inclusive sum over the wave's lanes: inside rows of 16 lanes, then the last lane of row 0 (2) to row 1 (3), that of row 1 to rows 2 and 3
+__device__ __forceinline__ int wave_sums(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);      // from 1, 2, 4, 8 lanes below
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
     return x;
 }
 // rows [lo, lo + len) of segment i, clamped, and its adapter (-1: none)
@@ -46,6 +47,17 @@ __device__ __forceinline__ void segment(const SegArgs& s, int i, int& lo, int& l
     }
 }
 
+// Asks for the scalar arguments that a kernel's start goes through one after the other, so that they come in one trip (the others are loaded where they
+// are needed).
+__device__ __forceinline__ void preload(const DownArgs& d) {
+    asm volatile("" :: "s"(d.seg.offsets), "s"(d.seg.ids), "s"(d.seg.n), "s"(d.seg.rows), "s"(d.seg.pool), "s"(d.n_steps), "s"(d.K), "s"(d.rank), "s"(d.splits));
+    asm volatile("" :: "s"(d.p[0]), "s"(d.f[0]), "s"(d.strides[0]), "s"(d.ldp[0]), "s"(d.ldf[0]), "s"(d.out), "s"(d.plane));
+}
+__device__ __forceinline__ void preload(const UpArgs& u) {
+    asm volatile("" :: "s"(u.seg.offsets), "s"(u.seg.ids), "s"(u.seg.n), "s"(u.seg.rows), "s"(u.seg.pool), "s"(u.f), "s"(u.stride), "s"(u.ldf), "s"(u.rank), "s"(u.cols));
+    asm volatile("" :: "s"(u.scale), "s"(u.c), "s"(u.ldc), "s"(u.bias), "s"(u.gelu), "s"(u.out), "s"(u.ldo), "s"(u.pre), "s"(u.v), "s"(u.v_out), "s"(u.tile));
+}
+
 struct Tile { int row0, rows, id; };
 // tile t of the tiles of at most T rows that the segments have, in their order; the same for every lane of a wave
 __device__ __forceinline__ bool find_tile(const SegArgs& s, int t, int T, Tile& out) {
@@ -54,7 +66,7 @@ __device__ __forceinline__ bool find_tile(const SegArgs& s, int t, int T, Tile& 
     for (int first = 0; first < s.n; first += 64) {
         int lo, len, id;
         segment(s, first + l, lo, len, id);
-        const int count = (len + T - 1) / T, sums = wave_sums(count, l);
+        const int count = (len + T - 1) / T, sums = wave_sums(count);
         const uint64_t behind = __ballot(base + sums > t);
         if (behind) {
             const int j = __builtin_ctzll(behind);
@@ -110,29 +122,41 @@ __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, cons
 constexpr int down_waves(int mt, int rb) { return mt + rb <= 5 ? 8 : 4; }
 template <int MT, int RB> struct DownShape {
     static constexpr int WAVES = down_waves(MT, RB);
-    static constexpr int X_BYTES = MT * 2048, SLOT = (MT + RB) * 2048, LOADS = 2 * (MT + RB);   // a unit: lines of 16 MT rows, of 16 RB ranks
+    static constexpr int SLOT = (MT + RB) * 2048;                                               // a unit: lines of 16 MT rows, of 16 RB ranks
     static constexpr int FIT = 163840 / (WAVES * SLOT), NS = FIT > 4 ? 4 : FIT;
     static constexpr int PART = 16 * RB + 4, SUMS = WAVES * 16 * PART * 4;                      // the waves' sums of 16 rows
     static constexpr int BYTES = WAVES * NS * SLOT > SUMS ? WAVES * NS * SLOT : SUMS;
     static_assert(NS >= 1 && BYTES <= 163840);
 };
-template <int MT, int RB, bool DROP>
-__global__ __launch_bounds__(64 * down_waves(MT, RB)) void tp_adapter_down_kernel(const DownArgs p) {
-    using Sh = DownShape<MT, RB>;
-    constexpr int WAVES = Sh::WAVES, NS = Sh::NS;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    Tile t;
-    if (!find_tile(p.seg, blockIdx.x, 16 * MT, t) || t.id < 0) return;
-    const int l = threadIdx.x & 63, c = l & 15, g = l >> 4, w = uni(threadIdx.x >> 6);
-    const int KT = (p.K + 63) / 64, total = p.n_steps * KT, shares = p.splits * WAVES, share = blockIdx.y * WAVES + w;
+// one wave's sums over units share, share + shares, ... of tile t: acc[i][j][e] is row 16 i + c, rank 16 j + 4 g + e.  Its ring begins at byte `mine`.
+// XL: loads of eight rows of P each that the tile needs (rows beyond them are whatever LDS holds; so are their sums, which nobody reads).
+template <int MT, int RB, int NS, bool DROP, int XL>
+__device__ __forceinline__ void down_sums(const DownArgs& p, const Tile& t, const int share, const int shares, const uint32_t mine, f32x4_t (&acc)[MT][RB]) {
+    constexpr int X_BYTES = MT * 2048, SLOT = (MT + RB) * 2048, LOADS = XL + 2 * RB;
+    const int l = threadIdx.x & 63, c = l & 15, g = l >> 4;
+    const int KT = (p.K + 63) / 64, total = p.n_steps * KT;
     Mask m;
     if constexpr (DROP) m = open_mask(p.drop);
-    const uint32_t mine = (uint32_t)(w * NS * Sh::SLOT);
     // rows of 128 bytes, 16-byte chunk q of row r at q ^ ((r >> 1) & 7): reads of one chunk of 16 rows lie in different banks
     const int lr = l >> 3;
-    auto load = [&](auto n_loads, const uint16_t* base, int64_t bytes, int ld, int k0, uint32_t dst) __attribute__((always_inline)) {
+    // (descriptors and leading dimensions stay in scalar registers until the step changes: asked for again for every unit, they took 0.4 us of it)
+    u32x4_t rx, rf;
+    int ldp = 0, ldf = 0;
+    auto describe = [&](const uint16_t* base, int64_t bytes) __attribute__((always_inline)) {
         const uint64_t at = reinterpret_cast<uint64_t>(base);
-        const u32x4_t rs = {(uint32_t)uni((int)(uint32_t)at), (uint32_t)uni((int)((uint32_t)(at >> 32) & 0xffffu)), (uint32_t)uni((int)(uint32_t)bytes), 0x00020000u};
+        return u32x4_t{(uint32_t)uni((int)(uint32_t)at), (uint32_t)uni((int)((uint32_t)(at >> 32) & 0xffffu)), (uint32_t)uni((int)(uint32_t)bytes), 0x00020000u};
+    };
+    auto open_step = [&](int s) __attribute__((always_inline)) {
+        if (s < p.n_steps) {
+            ldp = p.ldp[s];
+            ldf = p.ldf[s];
+            rx = describe(static_cast<const uint16_t*>(p.p[s]) + (int64_t)t.row0 * ldp, ((int64_t)(t.rows - 1) * ldp + p.K) * 2);
+            rf = describe(static_cast<const uint16_t*>(p.f[s]) + t.id * p.strides[s], ((int64_t)(p.rank - 1) * ldf + p.K) * 2);
+        } else {
+            rx[2] = rf[2] = 0;
+        }
+    };
+    auto load = [&](auto n_loads, const u32x4_t& rs, int ld, int k0, uint32_t dst) __attribute__((always_inline)) {
         static_for<decltype(n_loads)::value>([&](auto n_) __attribute__((always_inline)) {
             constexpr int n = decltype(n_)::value;
             const int r = 8 * n + lr, k = k0 + (((l & 7) ^ ((r >> 1) & 7)) << 3);
@@ -141,17 +165,18 @@ __global__ __launch_bounds__(64 * down_waves(MT, RB)) void tp_adapter_down_kerne
     };
     int f_step = 0, f_kt = share;                                        // the unit to fetch next
     while (f_kt >= KT && f_step < p.n_steps) { f_kt -= KT; ++f_step; }
+    rx = rf = u32x4_t{0u, 0u, 0u, 0x00020000u};
+    open_step(f_step);
     auto fetch = [&](int slot) __attribute__((always_inline)) {          // (past the end: empty descriptors, zeros that nobody uses)
-        const bool live = f_step < p.n_steps;
-        const int s = uni(live ? f_step : 0), ldp = uni(p.ldp[s]), ldf = uni(p.ldf[s]), k0 = uni(64 * f_kt);
-        const uint32_t dst = mine + (uint32_t)(slot * Sh::SLOT);
-        load(std::integral_constant<int, 2 * MT>{}, static_cast<const uint16_t*>(p.p[s]) + (int64_t)t.row0 * ldp,
-             live ? ((int64_t)(t.rows - 1) * ldp + p.K) * 2 : 0, ldp, k0, dst);
-        load(std::integral_constant<int, 2 * RB>{}, static_cast<const uint16_t*>(p.f[s]) + t.id * p.strides[s],
-             live ? ((int64_t)(p.rank - 1) * ldf + p.K) * 2 : 0, ldf, k0, dst + Sh::X_BYTES);
-        for (f_kt += shares; f_kt >= KT && f_step < p.n_steps; ++f_step) f_kt -= KT;
+        const uint32_t dst = mine + (uint32_t)(slot * SLOT);
+        load(std::integral_constant<int, XL>{}, rx, ldp, 64 * f_kt, dst);
+        load(std::integral_constant<int, 2 * RB>{}, rf, ldf, 64 * f_kt, dst + X_BYTES);
+        f_kt += shares;
+        if (f_kt >= KT && f_step < p.n_steps) {
+            do { f_kt -= KT; ++f_step; } while (f_kt >= KT && f_step < p.n_steps);
+            open_step(f_step);
+        }
     };
-    f32x4_t acc[MT][RB];                                                 // acc[i][j][e]: row 16 i + c, rank 16 j + 4 g + e
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -163,9 +188,9 @@ __global__ __launch_bounds__(64 * down_waves(MT, RB)) void tp_adapter_down_kerne
     for (int u = share; u < total; u += shares) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");               // the slot to refill has been read
         fetch(slot == 0 ? NS - 1 : slot - 1);
-        wait_vm<(NS - 1) * Sh::LOADS>();
+        wait_vm<(NS - 1) * LOADS>();
         asm volatile("" ::: "memory");
-        const uint32_t at = mine + (uint32_t)(slot * Sh::SLOT);
+        const uint32_t at = mine + (uint32_t)(slot * SLOT);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             auto frag = [&](uint32_t base, int i) __attribute__((always_inline)) {
@@ -174,7 +199,7 @@ __global__ __launch_bounds__(64 * down_waves(MT, RB)) void tp_adapter_down_kerne
             };
             bf16x8_t f[RB];
 #pragma unroll
-            for (int j = 0; j < RB; ++j) f[j] = frag(at + Sh::X_BYTES, j);
+            for (int j = 0; j < RB; ++j) f[j] = frag(at + X_BYTES, j);
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 u32x4_t x = __builtin_bit_cast(u32x4_t, frag(at, i));
@@ -188,6 +213,26 @@ __global__ __launch_bounds__(64 * down_waves(MT, RB)) void tp_adapter_down_kerne
         for (kt += shares; kt >= KT && step < p.n_steps; ++step) kt -= KT;
     }
     wait_vm<0>();                                                        // (zeros on their way into slots)
+}
+// four ranks from 4 q on of row `row` of 16 rows: the waves' sums in their order
+template <int PART, int WAVES>
+__device__ __forceinline__ f32x4_t waves_sum(const float* part, int row, int q) {
+    f32x4_t s = *reinterpret_cast<const f32x4_t*>(part + row * PART + 4 * q);
+#pragma unroll
+    for (int v = 1; v < WAVES; ++v) s += *reinterpret_cast<const f32x4_t*>(part + (v * 16 + row) * PART + 4 * q);
+    return s;
+}
+template <int MT, int RB, bool DROP>
+__global__ __launch_bounds__(64 * down_waves(MT, RB)) void tp_adapter_down_kernel(const DownArgs p) {
+    using Sh = DownShape<MT, RB>;
+    constexpr int WAVES = Sh::WAVES;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    preload(p);
+    Tile t;
+    if (!find_tile(p.seg, blockIdx.x, 16 * MT, t) || t.id < 0) return;
+    const int l = threadIdx.x & 63, c = l & 15, g = l >> 4, w = uni(threadIdx.x >> 6);
+    f32x4_t acc[MT][RB];
+    down_sums<MT, RB, Sh::NS, DROP, 2 * MT>(p, t, blockIdx.y * WAVES + w, p.splits * WAVES, (uint32_t)(w * Sh::NS * Sh::SLOT), acc);
     __syncthreads();
     float* const part = reinterpret_cast<float*>(lds);
     float* const out = p.out + blockIdx.y * p.plane;
@@ -200,9 +245,7 @@ __global__ __launch_bounds__(64 * down_waves(MT, RB)) void tp_adapter_down_kerne
         for (int x = threadIdx.x; x < 64 * RB; x += 64 * WAVES) {
             const int row = x / (4 * RB), q = x % (4 * RB);
             if (16 * i + row >= t.rows || 4 * q >= p.rank) continue;
-            f32x4_t s = *reinterpret_cast<const f32x4_t*>(part + row * Sh::PART + 4 * q);
-#pragma unroll
-            for (int v = 1; v < WAVES; ++v) s += *reinterpret_cast<const f32x4_t*>(part + (v * 16 + row) * Sh::PART + 4 * q);
+            f32x4_t s = waves_sum<Sh::PART, WAVES>(part, row, q);
             if constexpr (DROP) s *= p.drop.factor;
             *reinterpret_cast<f32x4_t*>(out + (int64_t)(t.row0 + 16 * i + row) * p.rank + 4 * q) = s;
         }
@@ -226,24 +269,27 @@ template <int GP, int TERMS> struct UpShape {
 };
 template <bool C32> struct CRows { u32x4_t v[4][C32 ? 2 : 1]; };
 template <int GP, int TERMS, bool DROP, bool C32>
-__global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
+struct UpStrip {
     using Sh = UpShape<GP, TERMS>;
-    constexpr bool AHEAD = Sh::template AHEAD<C32>;
-    constexpr bool O32 = TERMS == 3, WIDE = !C32 && !O32;
-    extern __shared__ __attribute__((aligned(16))) char low[];
-    const int l = threadIdx.x & 63, c = l & 15, g = l >> 4;
-    const int strip = uni(blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6));
-    Tile t;
-    if (!find_tile(p.seg, blockIdx.x, p.tile, t)) return;
-    const bool adapted = t.id >= 0;
+    static constexpr bool O32 = TERMS == 3, WIDE = !C32 && !O32;
+    static constexpr int CB = C32 ? 4 : 2;
+    const UpArgs& p;
+    const Tile& t;
+    int c, g, n;
+    bool in, in1;
     // the lane's columns: n .. n + 7, or n .. n + 3 and n + 64 .. n + 67
-    const int n = strip * 128 + (WIDE ? 8 : 4) * c;
-    const bool in = n < p.cols, in1 = WIDE ? in : n + 64 < p.cols;
+    __device__ __forceinline__ UpStrip(const UpArgs& args, const Tile& tile, int strip) : p(args), t(tile) {
+        const int l = threadIdx.x & 63;
+        c = l & 15;
+        g = l >> 4;
+        n = strip * 128 + (WIDE ? 8 : 4) * c;
+        in = n < p.cols;
+        in1 = WIDE ? in : n + 64 < p.cols;
+    }
     // C of rows r0 + 4 g + e (past the end: the last row; past the columns: the first ones)
-    constexpr int CB = C32 ? 4 : 2;
-    const char* const c0 = static_cast<const char*>(p.c) + (int64_t)t.row0 * p.ldc * CB;
-    const int at0 = (in ? n : 0) * CB, at1 = (in1 ? n + 64 : 0) * CB;
-    auto load_c = [&](CRows<C32>& q, int r0) __attribute__((always_inline)) {
+    __device__ __forceinline__ void load_c(CRows<C32>& q, int r0) const {
+        const char* const c0 = static_cast<const char*>(p.c) + (int64_t)t.row0 * p.ldc * CB;
+        const int at0 = (in ? n : 0) * CB, at1 = (in1 ? n + 64 : 0) * CB;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int r = r0 + 4 * g + e < t.rows ? r0 + 4 * g + e : t.rows - 1;
@@ -259,16 +305,50 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
                 q.v[e][0] = u32x4_t{a[0], a[1], b[0], b[1]};
             }
         }
-    };
-    // eight bf16 values of a row at `base` (16 bytes, or 8 and 8), and back
-    auto load_row = [&](const __amdgpu_buffer_rsrc_t& rs, int k, bool ok) __attribute__((always_inline)) {
-        const uint32_t at = (uint32_t)((k * p.ldf + n) * 2);
-        if constexpr (WIDE) return buf_load16(rs, ok && in ? at : OOB_OFFSET);
-        const u32x2_t a = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(ok && in ? at : OOB_OFFSET), 0, 0);
-        const u32x2_t b = __builtin_amdgcn_raw_buffer_load_b64(rs, (int)(ok && in1 ? at + 128 : OOB_OFFSET), 0, 0);
-        return u32x4_t{a[0], a[1], b[0], b[1]};
-    };
-    auto store_bf16 = [&](void* base, int64_t ld, int64_t row, const float (&v)[8]) __attribute__((always_inline)) {
+    }
+    // the strip of the factor, and its rows turned into matrix operands
+    __device__ __forceinline__ void load_factor(u32x4_t (&f)[Sh::NS][8]) const {
+        const __amdgpu_buffer_rsrc_t rf = make_rsrc(static_cast<const uint16_t*>(p.f) + t.id * p.stride, ((int64_t)(p.rank - 1) * p.ldf + p.cols) * 2);
+#pragma unroll
+        for (int s = 0; s < Sh::NS; ++s) {
+            const int k = 8 * (GP >= 4 ? 4 * s + g : g & (GP - 1));
+            const bool ok = k < p.rank;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t at = (uint32_t)(((k + j) * p.ldf + n) * 2);
+                if constexpr (WIDE) {
+                    f[s][j] = buf_load16(rf, ok && in ? at : OOB_OFFSET);
+                } else {
+                    const u32x2_t a = __builtin_amdgcn_raw_buffer_load_b64(rf, (int)(ok && in ? at : OOB_OFFSET), 0, 0);
+                    const u32x2_t b = __builtin_amdgcn_raw_buffer_load_b64(rf, (int)(ok && in1 ? at + 128 : OOB_OFFSET), 0, 0);
+                    f[s][j] = u32x4_t{a[0], a[1], b[0], b[1]};
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void turn(u32x4_t (&f)[Sh::NS][8]) const {
+#pragma unroll
+        for (int s = 0; s < Sh::NS; ++s) {
+            u32x4_t o[8];
+            transpose8(f[s], o);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[s][j] = o[j];
+        }
+    }
+    __device__ __forceinline__ u32x4_t load_bias() const {
+        u32x4_t bias = {0u, 0u, 0u, 0u};
+        if (p.bias) {
+            const char* const b = static_cast<const char*>(p.bias);
+            if constexpr (WIDE) {
+                bias = *reinterpret_cast<const u32x4_t*>(b + (in ? n : 0) * 2);
+            } else {
+                const u32x2_t q = *reinterpret_cast<const u32x2_t*>(b + (in ? n : 0) * 2), s = *reinterpret_cast<const u32x2_t*>(b + (in1 ? n + 64 : 0) * 2);
+                bias = u32x4_t{q[0], q[1], s[0], s[1]};
+            }
+        }
+        return bias;
+    }
+    __device__ __forceinline__ void store_bf16(void* base, int64_t ld, int64_t row, const float (&v)[8]) const {
         uint16_t* const to = static_cast<uint16_t*>(base) + row * ld + n;
         const u32x4_t o = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
         if constexpr (WIDE) {
@@ -277,76 +357,9 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
             if (in) __builtin_nontemporal_store(u32x2_t{o[0], o[1]}, reinterpret_cast<u32x2_t*>(to));
             if (in1) __builtin_nontemporal_store(u32x2_t{o[2], o[3]}, reinterpret_cast<u32x2_t*>(to + 64));
         }
-    };
-    u32x4_t f[Sh::NS][8];
-    CRows<C32> next;
-    if (adapted) {
-        const __amdgpu_buffer_rsrc_t rf = make_rsrc(static_cast<const uint16_t*>(p.f) + t.id * p.stride, ((int64_t)(p.rank - 1) * p.ldf + p.cols) * 2);
-#pragma unroll
-        for (int s = 0; s < Sh::NS; ++s) {
-            const int k = 8 * (GP >= 4 ? 4 * s + g : g & (GP - 1));
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[s][j] = load_row(rf, k + j, k < p.rank);
-        }
-        if constexpr (AHEAD) load_c(next, 0);
-        // V's terms; eight ranks of a row a thread
-        const float scale = (p.scale ? p.scale[t.id] : 1.0f) * (DROP ? p.drop.factor : 1.0f);
-        for (int i = threadIdx.x; i < t.rows * GP; i += blockDim.x) {
-            const int r = i / GP, q = i % GP;
-            float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (8 * q < p.rank) {
-                const int64_t at = (int64_t)(t.row0 + r) * p.rank + 8 * q;
-                for (int z = 0; z < p.splits; ++z) {
-                    const f32x4_t *src = reinterpret_cast<const f32x4_t*>(p.v + z * p.plane + at), a = src[0], b = src[1];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) { v[k] += a[k]; v[4 + k] += b[k]; }
-                }
-                if (p.v_out && blockIdx.y == 0) {
-                    f32x4_t* const to = reinterpret_cast<f32x4_t*>(p.v_out + at);
-                    to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
-                    to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
-                }
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] *= scale;
-            }
-            u32x4_t term[TERMS];
-            split_terms(v, term);
-#pragma unroll
-            for (int s = 0; s < TERMS; ++s) *reinterpret_cast<u32x4_t*>(low + r * Sh::ROW + (s * GP + q) * 16) = term[s];
-            if constexpr (Sh::STEPS * 4 > TERMS * GP) *reinterpret_cast<u32x4_t*>(low + r * Sh::ROW + (TERMS * GP + q) * 16) = u32x4_t{0u, 0u, 0u, 0u};
-        }
-#pragma unroll
-        for (int s = 0; s < Sh::NS; ++s) {
-            u32x4_t o[8];
-            transpose8(f[s], o);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[s][j] = o[j];
-        }
-    } else if constexpr (AHEAD) {
-        load_c(next, 0);
     }
-    __syncthreads();
-    if (strip * 128 >= p.cols) return;
-    Mask m;
-    if constexpr (DROP) m = open_mask(p.drop);
-    u32x4_t bias = {0u, 0u, 0u, 0u};
-    if (p.bias) {
-        const char* const b = static_cast<const char*>(p.bias);
-        if constexpr (WIDE) {
-            bias = *reinterpret_cast<const u32x4_t*>(b + (in ? n : 0) * 2);
-        } else {
-            const u32x2_t q = *reinterpret_cast<const u32x2_t*>(b + (in ? n : 0) * 2), s = *reinterpret_cast<const u32x2_t*>(b + (in1 ? n + 64 : 0) * 2);
-            bias = u32x4_t{q[0], q[1], s[0], s[1]};
-        }
-    }
-    for (int r0 = 0; r0 < t.rows; r0 += 16) {
-        CRows<C32> cv;
-        if constexpr (AHEAD) {
-            cv = next;
-            if (r0 + 16 < t.rows) load_c(next, r0 + 16);
-        } else {
-            load_c(cv, r0);
-        }
+    // rows r0 .. r0 + 15 of the tile from V's terms at `low` (adapted) and their C
+    __device__ __forceinline__ void rows16(const char* low, const u32x4_t (&f)[Sh::NS][8], const CRows<C32>& cv, const u32x4_t& bias, const Mask& m, int r0, bool adapted) const {
         f32x4_t acc[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -397,6 +410,155 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
             }
         }
     }
+};
+// eight ranks' terms of row r, group q of V (already scaled), to LDS
+template <int GP, int TERMS>
+__device__ __forceinline__ void lay_terms(char* low, int r, int q, const float (&v)[8]) {
+    using Sh = UpShape<GP, TERMS>;
+    u32x4_t term[TERMS];
+    split_terms(v, term);
+#pragma unroll
+    for (int s = 0; s < TERMS; ++s) *reinterpret_cast<u32x4_t*>(low + r * Sh::ROW + (s * GP + q) * 16) = term[s];
+    if constexpr (Sh::STEPS * 4 > TERMS * GP) *reinterpret_cast<u32x4_t*>(low + r * Sh::ROW + (TERMS * GP + q) * 16) = u32x4_t{0u, 0u, 0u, 0u};
+}
+
+template <int GP, int TERMS, bool DROP, bool C32>
+__global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
+    using Strip = UpStrip<GP, TERMS, DROP, C32>;
+    constexpr bool AHEAD = UpShape<GP, TERMS>::template AHEAD<C32>;
+    extern __shared__ __attribute__((aligned(16))) char low[];
+    const int strip = uni(blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6));
+    preload(p);
+    Tile t;
+    if (!find_tile(p.seg, blockIdx.x, p.tile, t)) return;
+    const bool adapted = t.id >= 0;
+    const Strip st(p, t, strip);
+    u32x4_t f[UpShape<GP, TERMS>::NS][8];
+    CRows<C32> next;
+    if (adapted) {
+        st.load_factor(f);
+        if constexpr (AHEAD) st.load_c(next, 0);
+        // V's terms; eight ranks of a row a thread
+        const float scale = (p.scale ? p.scale[t.id] : 1.0f) * (DROP ? p.drop.factor : 1.0f);
+        for (int i = threadIdx.x; i < t.rows * GP; i += blockDim.x) {
+            const int r = i / GP, q = i % GP;
+            float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (8 * q < p.rank) {
+                const int64_t at = (int64_t)(t.row0 + r) * p.rank + 8 * q;
+                for (int z = 0; z < p.splits; ++z) {
+                    const f32x4_t *src = reinterpret_cast<const f32x4_t*>(p.v + z * p.plane + at), a = src[0], b = src[1];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) { v[k] += a[k]; v[4 + k] += b[k]; }
+                }
+                if (p.v_out && blockIdx.y == 0) {
+                    f32x4_t* const to = reinterpret_cast<f32x4_t*>(p.v_out + at);
+                    to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+                    to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] *= scale;
+            }
+            lay_terms<GP, TERMS>(low, r, q, v);
+        }
+        st.turn(f);
+    } else if constexpr (AHEAD) {
+        st.load_c(next, 0);
+    }
+    __syncthreads();
+    if (strip * 128 >= p.cols) return;
+    Mask m;
+    if constexpr (DROP) m = open_mask(p.drop);
+    const u32x4_t bias = st.load_bias();
+    for (int r0 = 0; r0 < t.rows; r0 += 16) {
+        CRows<C32> cv;
+        if constexpr (AHEAD) {
+            cv = next;
+            if (r0 + 16 < t.rows) st.load_c(next, r0 + 16);
+        } else {
+            st.load_c(cv, r0);
+        }
+        st.rows16(low, f, cv, bias, m, r0, adapted);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// few.  Both products of a tile of 16 rows in one launch, for segments of a few rows (a decoding batch): every workgroup of a tile forms V by itself, its waves
+// sharing K, and goes on with its own strips.  The factor's first strip and C come in meanwhile.  Bound by latency: a launch, one trip for the
+// segment, one for the operands; with many requests by the factors.  What is read more than once is A, once for every workgroup of
+// a tile, from L2.
+// ---------------------------------------------------------------------------------------------
+constexpr int few_waves(int rb) { return rb <= 4 ? 8 : 4; }              // (as many as leave a wave its registers)
+template <int RB> struct FewShape {                                      // RB: blocks of 16 ranks
+    static constexpr int WAVES = few_waves(RB), SLOT = (1 + RB) * 2048, FIT = 163840 / (WAVES * SLOT), NS = FIT > 4 ? 4 : FIT;
+    static constexpr int PART = 16 * RB + 4, SUMS = WAVES * 16 * PART * 4;
+    static constexpr int LOW = 16 * UpShape<2 * RB, 3>::ROW;             // behind the waves' sums, where the ring was
+    static constexpr int BYTES = WAVES * NS * SLOT > SUMS + LOW ? WAVES * NS * SLOT : SUMS + LOW;
+    static_assert(NS >= 1 && BYTES <= 163840);
+};
+template <int RB, int TERMS, bool C32>
+__global__ __launch_bounds__(64 * few_waves(RB)) void tp_adapter_few_kernel(const DownArgs d, const UpArgs p) {
+    constexpr int GP = 2 * RB;
+    using Sh = FewShape<RB>;
+    using Strip = UpStrip<GP, TERMS, false, C32>;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int l = threadIdx.x & 63, c = l & 15, g = l >> 4, w = uni(threadIdx.x >> 6);
+    preload(p);
+    preload(d);
+    Tile t;
+    if (!find_tile(p.seg, blockIdx.x, 16, t)) return;
+    const bool adapted = t.id >= 0;
+    const int strips = (p.cols + 127) / 128, step = gridDim.y * Sh::WAVES;
+    int strip = blockIdx.y * Sh::WAVES + w;
+    constexpr int EARLY = RB <= 2 ? 2 : 1;                               // strips whose factor comes in early
+    u32x4_t f[EARLY][UpShape<GP, TERMS>::NS][8];
+    CRows<C32> cv;
+    char* const low = lds + Sh::SUMS;
+    if (adapted) {
+#pragma unroll
+        for (int s = 0; s < EARLY; ++s)
+            if (strip + s * step < strips) Strip(p, t, strip + s * step).load_factor(f[s]);
+    }
+    if (adapted) {
+        const float scale = p.scale ? p.scale[t.id] : 1.0f;
+        f32x4_t acc[1][RB];
+        const uint32_t ring = (uint32_t)(w * Sh::NS * Sh::SLOT);
+        if (t.rows <= 8) down_sums<1, RB, Sh::NS, false, 1>(d, t, w, Sh::WAVES, ring, acc);
+        else             down_sums<1, RB, Sh::NS, false, 2>(d, t, w, Sh::WAVES, ring, acc);
+        if (strip < strips) Strip(p, t, strip).load_c(cv, 0);
+        __syncthreads();
+        float* const part = reinterpret_cast<float*>(lds);
+#pragma unroll
+        for (int j = 0; j < RB; ++j) *reinterpret_cast<f32x4_t*>(part + (w * 16 + c) * Sh::PART + 16 * j + 4 * g) = acc[0][j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < t.rows * GP; i += 64 * Sh::WAVES) {
+            const int r = i / GP, q = i % GP;
+            const f32x4_t a = waves_sum<Sh::PART, Sh::WAVES>(part, r, 2 * q), b = waves_sum<Sh::PART, Sh::WAVES>(part, r, 2 * q + 1);
+            if (p.v_out && blockIdx.y == 0 && 8 * q < p.rank) {
+                f32x4_t* const to = reinterpret_cast<f32x4_t*>(p.v_out + (int64_t)(t.row0 + r) * p.rank + 8 * q);
+                to[0] = a;
+                to[1] = b;
+            }
+            const float v[8] = {a[0] * scale, a[1] * scale, a[2] * scale, a[3] * scale, b[0] * scale, b[1] * scale, b[2] * scale, b[3] * scale};
+            lay_terms<GP, TERMS>(low, r, q, v);
+        }
+        __syncthreads();
+    }
+    Mask none{};
+#pragma unroll
+    for (int s = 0; s < EARLY; ++s, strip += step) {
+        if (strip >= strips) return;
+        const Strip st(p, t, strip);
+        if (s || !adapted) st.load_c(cv, 0);
+        if (adapted) st.turn(f[s]);
+        st.rows16(low, f[s], cv, st.load_bias(), none, 0, adapted);
+    }
+    for (; strip < strips; strip += step) {
+        const Strip st(p, t, strip);
+        if (adapted) st.load_factor(f[0]);
+        st.load_c(cv, 0);
+        if (adapted) st.turn(f[0]);
+        st.rows16(low, f[0], cv, st.load_bias(), none, 0, adapted);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -426,7 +588,7 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
         int lo, len, id;
         segment(p.seg, first + l, lo, len, id);
         const int count = id == a ? (len + 31) / 32 : 0;
-        total += __builtin_amdgcn_readlane(wave_sums(count, l), 63);
+        total += __builtin_amdgcn_readlane(wave_sums(count), 63);
     }
     if (p.shares > 1 && share == 0 && strip_all == 0 && rank0 == 0 && threadIdx.x == 0) p.units[a] = total;
     const int u0 = (int)((int64_t)total * share / p.shares), u1 = (int)((int64_t)total * (share + 1) / p.shares);
@@ -479,7 +641,7 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
     for (int first = 0; first < p.seg.n && base < u1; first += 64) {
         int lo, len, id;
         segment(p.seg, first + l, lo, len, id);
-        const int count = id == a ? (len + 31) / 32 : 0, sums = wave_sums(count, l);
+        const int count = id == a ? (len + 31) / 32 : 0, sums = wave_sums(count);
         for (uint64_t some = __ballot(count > 0); some; some &= some - 1) {
             const int j = __builtin_ctzll(some);
             const int units = __builtin_amdgcn_readlane(count, j), before = base + __builtin_amdgcn_readlane(sums, j) - units;
@@ -599,6 +761,27 @@ hipError_t launch_down(const DownArgs& a, hipStream_t s) {
         case 64: return down_rank<4>(a, s);
         default: return hipErrorInvalidValue;
     }
+}
+
+template <int RB, int TERMS, bool C32>
+static hipError_t few(const DownArgs& d, const UpArgs& u, hipStream_t s) {
+    using Sh = FewShape<RB>;
+    static std::atomic<uint64_t> done{0};
+    if (hipError_t e = allow_lds(tp_adapter_few_kernel<RB, TERMS, C32>, Sh::BYTES, done); e != hipSuccess) return e;
+    // workgroups of a tile: while there are CUs for them, as many as leave a wave one strip
+    const int strips = (u.cols + 127) / 128, most = (strips + Sh::WAVES - 1) / Sh::WAVES, room = u.tiles < 256 ? 256 / u.tiles : 1;
+    return launch_kernel(tp_adapter_few_kernel<RB, TERMS, C32>, dim3((unsigned)u.tiles, (unsigned)(most < room ? most : room)), dim3(64 * Sh::WAVES), Sh::BYTES, s,
+                         d, u);
+}
+hipError_t launch_few(const DownArgs& d, const UpArgs& u, hipStream_t s) {
+    if (d.dropped || u.dropped || u.tile != 16) return hipErrorInvalidValue;
+    auto pick = [&](auto rb) {
+        constexpr int RB = decltype(rb)::value;
+        if (u.out_f32) return u.c_f32 ? few<RB, 3, true>(d, u, s) : few<RB, 3, false>(d, u, s);
+        return u.c_f32 ? few<RB, 2, true>(d, u, s) : few<RB, 2, false>(d, u, s);
+    };
+    return u.rank <= 16 ? pick(std::integral_constant<int, 1>{}) : u.rank <= 32 ? pick(std::integral_constant<int, 2>{})
+         : u.rank <= 64 ? pick(std::integral_constant<int, 4>{}) : pick(std::integral_constant<int, 8>{});
 }
 
 hipError_t launch_up(const UpArgs& a, hipStream_t s) {

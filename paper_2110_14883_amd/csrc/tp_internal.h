@@ -115,7 +115,9 @@ struct UpArgs {
     DropArgs drop;
 };
 hipError_t launch_up(const UpArgs& args, hipStream_t stream);
-// Waves of a workgroup there, a strip of 128 columns each: as few idle ones as possible, about four; with few tiles a strip a workgroup
+// Both in one launch, without dropout, tiles of 16 rows (V is not kept but for v_out)
+hipError_t launch_few(const DownArgs& down, const UpArgs& up, hipStream_t stream);
+// Waves of a workgroup of launch_up, a strip of 128 columns each: as few idle ones as possible, about four; with few tiles a strip a workgroup
 inline int up_waves(int strips, int64_t tiles) {
     if (tiles * ((strips + 3) / 4) < 256) return 1;
     int best = 4;

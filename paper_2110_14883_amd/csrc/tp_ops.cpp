@@ -103,6 +103,8 @@ Split plan_products(int64_t rows, int64_t segments, int64_t k, int n_steps, int6
     s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / s.tiles, units / 8, 16}));
     return s;
 }
+// Elements of a factor up to which both products of a short segment go into one launch, where every workgroup of a tile reads it whole
+constexpr int64_t kFewFactor = (int64_t)1 << 20;
 // Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) for two a CU (four: 63 us for 55, and more planes), 128 rows a share at least
 int plan_grad(int64_t rows, int64_t cols, int pool, int rank) {
     const int64_t blocks = (cols + 127) / 128 * ((rank + 63) / 64) * pool;
@@ -197,12 +199,14 @@ int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
         if (int e = check_oblk(preact, s.n, false)) return e;
         if (preact.dtype != TP_BF16) return TP_ERR_DTYPE;
     }
-    u.v = planes; u.v_out = planes == v ? nullptr : v;
+    const bool few = sp.tile == 16 && !drop && (int64_t)n_steps * s.k * adapters->rank <= kFewFactor;
+    u.v = planes; u.v_out = planes == v && !few ? nullptr : v;
     u.bias = epi == TP_EPI_NONE ? nullptr : bias; u.gelu = epi == TP_EPI_BIAS_GELU;
     u.pre = preact.ptr; u.ldp = preact.ld;
     if (!ws_ok(need.all(), workspace, workspace_bytes)) return TP_ERR_WORKSPACE;
     if (adapters->n_segments == 0) return TP_OK;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (few) return launch_few(d, u, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
     return launch_down(d, stream) != hipSuccess || launch_up(u, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
 }
 
