@@ -18,6 +18,7 @@ namespace {
 
 PyObject *s_data_ptr, *s_stride, *s_shape, *s_dtype, *s_numel, *s_element_size;      // interned names
 PyObject *s_get_device, *s_is_contiguous;
+PyObject* g_tensor;                                                                  // torch.Tensor, or None
 PyObject *g_i32, *g_f32, *g_bf16;                                                            // torch.int32, torch.float32, torch.bfloat16
 PyObject *g_current_device;                                                          // callable, or None: its answer is not compared
 
@@ -64,9 +65,10 @@ bool call0(PyObject* o, PyObject* name, int64_t* out) {
     return r && to_i64(r.p, out);
 }
 bool is_sequence(PyObject* o) { return PyTuple_Check(o) || PyList_Check(o); }
-// a tensor has data_ptr; what has none is taken as a sequence
+// a tensor has data_ptr; what has none is taken as a sequence.  (torch's own types are known without asking.)
 bool is_tensor(PyObject* o, bool* yes) {
     if (is_sequence(o)) { *yes = false; return true; }
+    if (g_tensor && (PyObject*)Py_TYPE(o) == g_tensor) { *yes = true; return true; }
     Ref a(PyObject_GetAttr(o, s_data_ptr));
     if (!a && !PyErr_ExceptionMatches(PyExc_AttributeError)) return false;
     *yes = (bool)a;
@@ -74,6 +76,7 @@ bool is_tensor(PyObject* o, bool* yes) {
     return true;
 }
 bool item(PyObject* o, Py_ssize_t i, int64_t* out) {
+    if (PyTuple_CheckExact(o) && i < PyTuple_GET_SIZE(o)) return to_i64(PyTuple_GET_ITEM(o, i), out);
     Ref v(PySequence_GetItem(o, i));
     return v && to_i64(v.p, out);
 }
@@ -330,6 +333,62 @@ bool look(PyObject* o, PyObject* want, Devices* at) {
     return false;
 }
 
+// A block: None, a sequence as to_oblk() and to_cblk() take it, or a tensor on the current device of type `want` (null: fp32 or bf16, else 99)
+bool to_block(PyObject* o, PyObject* want, Devices* at, tp_oblk_t* b) {
+    bool tensor = false;
+    if (o == Py_None) return to_oblk(o, b);
+    if (!is_tensor(o, &tensor)) return false;
+    if (!tensor) {
+        if (!want) return to_oblk(o, b);
+        tp_cblk_t c;
+        if (!to_cblk(o, &c)) return false;
+        *b = tp_oblk_t{const_cast<void*>(c.ptr), c.ld, 0};
+        return true;
+    }
+    int64_t ptr = 0, ld = 0;
+    if (!at->add(o) || !call0(o, s_data_ptr, &ptr) || !tensor_ld(o, &ld)) return false;
+    Ref dt(PyObject_GetAttr(o, s_dtype));
+    if (!dt) return false;
+    if (want && want != Py_None && dt.p != want) {
+        PyErr_Format(PyExc_TypeError, "%R expected, got %R", want, dt.p);
+        return false;
+    }
+    *b = tp_oblk_t{reinterpret_cast<void*>(ptr), ld, dt.p == g_f32 ? TP_F32 : dt.p == g_bf16 ? TP_BF16 : 99};
+    return true;
+}
+bool to_input(PyObject* o, Devices* at, tp_cblk_t* b) {           // bf16
+    tp_oblk_t q;
+    if (!to_block(o, g_bf16, at, &q)) return false;
+    *b = tp_cblk_t{q.ptr, q.ld};
+    return true;
+}
+struct Inputs {                                                  // a list of them, with empty ones up to TP_MAX_STEPS; None: a null pointer
+    tp_cblk_t blocks[TP_MAX_STEPS] = {};
+    const tp_cblk_t* ptr = nullptr;
+    bool fill(PyObject* o, Devices* at) {
+        if (o == Py_None) return true;
+        if (PyObject_Size(o) < 0) return false;
+        Ref s(PySequence_Fast(o, "blocks must be a sequence"));
+        if (!s) return false;
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(s.p);
+        if (n > TP_MAX_STEPS) { PyErr_SetString(PyExc_ValueError, "too many blocks"); return false; }
+        for (Py_ssize_t i = 0; i < n; ++i)
+            if (!to_input(PySequence_Fast_GET_ITEM(s.p, i), at, blocks + i)) return false;
+        ptr = blocks;
+        return true;
+    }
+};
+struct MaybeInput {
+    tp_cblk_t b;
+    const tp_cblk_t* ptr = nullptr;
+    bool fill(PyObject* o, Devices* at) {
+        if (o == Py_None) return true;
+        if (!to_input(o, at, &b)) return false;
+        ptr = &b;
+        return true;
+    }
+};
+
 // A mask: a sequence (p, seed, offset, offset_dev, row0, col0)
 bool to_dropout(PyObject* o, tp_dropout_t* d, Devices* at) {
     Ref s(PySequence_Fast(o, "dropout must be a Dropout"));
@@ -352,17 +411,16 @@ bool to_dropout(PyObject* o, tp_dropout_t* d, Devices* at) {
 // dropout_fwd(dropout, x, bias, epi, residual, y, preact, rows, cols, stream)
 PyObject* dropout_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     tp_dropout_t d; tp_oblk_t x, y, pre; tp_cblk_t res; void *bias, *stream; int epi; int64_t rows, cols; Devices at;
-    if (!count(n, 10) || !look(a[1], nullptr, &at) || !look(a[2], g_bf16, &at) || !look(a[4], g_bf16, &at) || !look(a[5], nullptr, &at) ||
-        !look(a[6], nullptr, &at) || !to_dropout(a[0], &d, &at) || !to_oblk(a[1], &x) || !to_ptr(a[2], &bias) || !to_int(a[3], &epi) || !to_cblk(a[4], &res) ||
-        !to_oblk(a[5], &y) || !to_oblk(a[6], &pre) || !to_i64(a[7], &rows) || !to_i64(a[8], &cols) || !to_ptr(a[9], &stream))
+    if (!count(n, 10) || !to_dropout(a[0], &d, &at) || !to_block(a[1], nullptr, &at, &x) || !look(a[2], g_bf16, &at) || !to_ptr(a[2], &bias) ||
+        !to_int(a[3], &epi) || !to_input(a[4], &at, &res) || !to_block(a[5], nullptr, &at, &y) || !to_block(a[6], nullptr, &at, &pre) || !to_i64(a[7], &rows) || !to_i64(a[8], &cols) || !to_ptr(a[9], &stream))
         return nullptr;
     return answer([&] { return f_dropout_fwd(&d, x.ptr, x.ld, x.dtype, bias, epi, res, y, pre, rows, cols, stream); });
 }
 // dropout_bwd(dropout, dy, preact, dx, db, rows, cols, workspace, stream)
 PyObject* dropout_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     tp_dropout_t d; tp_cblk_t dy, pre, dx; void *db, *stream; int64_t rows, cols; Workspace ws; Devices at;
-    if (!count(n, 9) || !look(a[1], g_bf16, &at) || !look(a[2], g_bf16, &at) || !look(a[3], g_bf16, &at) || !look(a[4], g_f32, &at) ||
-        !look(a[7], nullptr, &at) || !to_dropout(a[0], &d, &at) || !to_cblk(a[1], &dy) || !to_cblk(a[2], &pre) || !to_cblk(a[3], &dx) || !to_ptr(a[4], &db) ||
+    if (!count(n, 9) || !look(a[4], g_f32, &at) || !look(a[7], nullptr, &at) || !to_dropout(a[0], &d, &at) || !to_input(a[1], &at, &dy) ||
+        !to_input(a[2], &at, &pre) || !to_input(a[3], &at, &dx) || !to_ptr(a[4], &db) ||
         !to_i64(a[5], &rows) || !to_i64(a[6], &cols) || !to_ws(a[7], &ws) || !to_ptr(a[8], &stream))
         return nullptr;
     return answer([&] {
@@ -446,14 +504,6 @@ struct Factors {
         return true;
     }
 };
-bool look_all(PyObject* o, PyObject* want, Devices* at) {
-    if (o == Py_None || PyObject_Size(o) < 0) return !PyErr_Occurred();
-    Ref s(PySequence_Fast(o, "blocks must be a sequence"));
-    if (!s) return false;
-    for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(s.p); ++i)
-        if (!look(PySequence_Fast_GET_ITEM(s.p, i), want, at)) return false;
-    return true;
-}
 // V: fp32 [rows, rank], one row behind the other
 bool to_v(PyObject* o, float** v, Devices* at) {
     void* p;
@@ -478,12 +528,12 @@ struct MaybeDropout {
 };
 // adapter_fwd(grid, dims, n_steps, adapters, x_blocks, a_blocks, b, dropout, c, bias, epi, y, preact, v, workspace, stream)
 PyObject* adapter_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    const tp_grid_t* grid; tp_dims_t dims; int steps, epi; tp_adapters_t ad; CBlocks x; Factors f; tp_factor_t b; MaybeDropout drop; tp_oblk_t c, y, pre;
+    const tp_grid_t* grid; tp_dims_t dims; int steps, epi; tp_adapters_t ad; Inputs x; Factors f; tp_factor_t b; MaybeDropout drop; tp_oblk_t c, y, pre;
     void *bias, *stream; float* v; Workspace ws; Devices at;
     if (!count(n, 16) || !to_struct(a[0], &grid) || !to_dims(a[1], &dims) || !to_int(a[2], &steps) || !to_adapters(a[3], &ad, &at) ||
-        !look_all(a[4], g_bf16, &at) || !x.fill(a[4]) || !f.fill(a[5], ad, &at) || !to_factor(a[6], &b, ad, g_bf16, &at) || !drop.fill(a[7], &at) ||
-        !look(a[8], nullptr, &at) || !to_oblk(a[8], &c) || !look(a[9], g_bf16, &at) || !to_ptr(a[9], &bias) || !to_int(a[10], &epi) ||
-        !look(a[11], nullptr, &at) || !to_oblk(a[11], &y) || !look(a[12], nullptr, &at) || !to_oblk(a[12], &pre) || !to_v(a[13], &v, &at) ||
+        !x.fill(a[4], &at) || !f.fill(a[5], ad, &at) || !to_factor(a[6], &b, ad, g_bf16, &at) || !drop.fill(a[7], &at) ||
+        !to_block(a[8], nullptr, &at, &c) || !look(a[9], g_bf16, &at) || !to_ptr(a[9], &bias) || !to_int(a[10], &epi) ||
+        !to_block(a[11], nullptr, &at, &y) || !to_block(a[12], nullptr, &at, &pre) || !to_v(a[13], &v, &at) ||
         !look(a[14], nullptr, &at) || !to_ws(a[14], &ws) || !to_ptr(a[15], &stream))
         return nullptr;
     return answer([&] {
@@ -492,12 +542,12 @@ PyObject* adapter_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 // adapter_bwd(grid, dims, n_steps, adapters, dy_blocks, b_blocks, a, dropout, dx_base, dx, x_own, da, dy_own, v, db, accumulate, workspace, stream)
 PyObject* adapter_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    const tp_grid_t* grid; tp_dims_t dims; int steps, accumulate; tp_adapters_t ad; CBlocks dy; Factors f; tp_factor_t fa; MaybeDropout drop;
-    tp_oblk_t base, dx; MaybeBlock x, own; tp_factor_out_t da, db; float* v; void* stream; Workspace ws; Devices at;
+    const tp_grid_t* grid; tp_dims_t dims; int steps, accumulate; tp_adapters_t ad; Inputs dy; Factors f; tp_factor_t fa; MaybeDropout drop;
+    tp_oblk_t base, dx; MaybeInput x, own; tp_factor_out_t da, db; float* v; void* stream; Workspace ws; Devices at;
     if (!count(n, 18) || !to_struct(a[0], &grid) || !to_dims(a[1], &dims) || !to_int(a[2], &steps) || !to_adapters(a[3], &ad, &at) ||
-        !look_all(a[4], g_bf16, &at) || !dy.fill(a[4]) || !f.fill(a[5], ad, &at) || !to_factor(a[6], &fa, ad, g_bf16, &at) || !drop.fill(a[7], &at) ||
-        !look(a[8], nullptr, &at) || !to_oblk(a[8], &base) || !look(a[9], nullptr, &at) || !to_oblk(a[9], &dx) || !look(a[10], g_bf16, &at) || !x.fill(a[10]) ||
-        !to_factor(a[11], &da, ad, g_f32, &at) || !look(a[12], g_bf16, &at) || !own.fill(a[12]) || !to_v(a[13], &v, &at) ||
+        !dy.fill(a[4], &at) || !f.fill(a[5], ad, &at) || !to_factor(a[6], &fa, ad, g_bf16, &at) || !drop.fill(a[7], &at) ||
+        !to_block(a[8], nullptr, &at, &base) || !to_block(a[9], nullptr, &at, &dx) || !x.fill(a[10], &at) ||
+        !to_factor(a[11], &da, ad, g_f32, &at) || !own.fill(a[12], &at) || !to_v(a[13], &v, &at) ||
         !to_factor(a[14], &db, ad, g_f32, &at) || !to_int(a[15], &accumulate) || !look(a[16], nullptr, &at) || !to_ws(a[16], &ws) || !to_ptr(a[17], &stream))
         return nullptr;
     return answer([&] {
@@ -523,14 +573,15 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-// bind_ops(addresses of the functions behind those, torch.int32, a function that gives the current device or None)
+// bind_ops(addresses of the functions behind those, torch.int32, torch.Tensor, a function that gives the current device or None)
 PyObject* bind_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* f[4];
-    if (!count(n, 6)) return nullptr;
+    if (!count(n, 7)) return nullptr;
     for (int i = 0; i < 4; ++i)
         if (!to_ptr(a[i], &f[i])) return nullptr;
     Py_INCREF(a[4]); Py_XSETREF(g_i32, a[4]);
-    Py_INCREF(a[5]); Py_XSETREF(g_current_device, a[5]);
+    Py_INCREF(a[5]); Py_XSETREF(g_tensor, a[5]);
+    Py_INCREF(a[6]); Py_XSETREF(g_current_device, a[6]);
     f_adapter_fwd = reinterpret_cast<decltype(f_adapter_fwd)>(f[2]);
     f_adapter_bwd = reinterpret_cast<decltype(f_adapter_bwd)>(f[3]);
     f_dropout_fwd = reinterpret_cast<decltype(f_dropout_fwd)>(f[0]);
