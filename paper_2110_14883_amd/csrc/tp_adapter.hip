@@ -265,7 +265,9 @@ template <int GP, int TERMS> struct UpShape {
     static constexpr int NS = GP >= 4 ? GP / 4 : 1;                      // blocks of 32 k that the factor has
     static constexpr int STEPS = (TERMS * GP + 3) / 4;                   // and V's terms
     static constexpr int ROW = STEPS * 64 + 16;                          // bytes of a row in LDS (16 more: rows start in different banks)
-    template <bool C32> static constexpr bool AHEAD = GP < 16 || !C32;   // whether there are registers for the next rows of C
+    // How many times 16 rows of C are on their way while others are finished: what leaves the waves that run without (two where two a SIMD fit anyway: 2048 x
+    // 8192, 64 ranks 19.6 -> 18.6 us; three instead of four waves a SIMD for it: 32896 x 640, 8 ranks 19.6 -> 23.8)
+    template <bool C32> static constexpr int AHEAD = C32 ? (GP < 16 ? 1 : 0) : (GP == 8 ? 2 : 1);
 };
 template <bool C32> struct CRows { u32x4_t v[4][C32 ? 2 : 1]; };
 template <int GP, int TERMS, bool DROP, bool C32>
@@ -425,7 +427,7 @@ __device__ __forceinline__ void lay_terms(char* low, int r, int q, const float (
 template <int GP, int TERMS, bool DROP, bool C32>
 __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
     using Strip = UpStrip<GP, TERMS, DROP, C32>;
-    constexpr bool AHEAD = UpShape<GP, TERMS>::template AHEAD<C32>;
+    constexpr int AHEAD = UpShape<GP, TERMS>::template AHEAD<C32>;
     extern __shared__ __attribute__((aligned(16))) char low[];
     const int strip = uni(blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6));
     preload(p);
@@ -434,10 +436,14 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
     const bool adapted = t.id >= 0;
     const Strip st(p, t, strip);
     u32x4_t f[UpShape<GP, TERMS>::NS][8];
-    CRows<C32> next;
+    CRows<C32> cv[AHEAD ? AHEAD : 1];
+    auto start_c = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) st.load_c(cv[i], 16 * i);
+    };
     if (adapted) {
         st.load_factor(f);
-        if constexpr (AHEAD) st.load_c(next, 0);
+        start_c();
         // V's terms; eight ranks of a row a thread
         const float scale = (p.scale ? p.scale[t.id] : 1.0f) * (DROP ? p.drop.factor : 1.0f);
         for (int i = threadIdx.x; i < t.rows * GP; i += blockDim.x) {
@@ -461,23 +467,29 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
             lay_terms<GP, TERMS>(low, r, q, v);
         }
         st.turn(f);
-    } else if constexpr (AHEAD) {
-        st.load_c(next, 0);
+    } else {
+        start_c();
     }
     __syncthreads();
     if (strip * 128 >= p.cols) return;
     Mask m;
     if constexpr (DROP) m = open_mask(p.drop);
     const u32x4_t bias = st.load_bias();
-    for (int r0 = 0; r0 < t.rows; r0 += 16) {
-        CRows<C32> cv;
-        if constexpr (AHEAD) {
-            cv = next;
-            if (r0 + 16 < t.rows) st.load_c(next, r0 + 16);
-        } else {
-            st.load_c(cv, r0);
+    if constexpr (AHEAD) {
+        for (int r0 = 0; r0 < t.rows; r0 += 16 * AHEAD)
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int r = r0 + 16 * i;
+                if (r >= t.rows) return;
+                const CRows<C32> now = cv[i];
+                if (r + 16 * AHEAD < t.rows) st.load_c(cv[i], r + 16 * AHEAD);
+                st.rows16(low, f, now, bias, m, r, adapted);
+            }
+    } else {
+        for (int r0 = 0; r0 < t.rows; r0 += 16) {
+            st.load_c(cv[0], r0);
+            st.rows16(low, f, cv[0], bias, m, r0, adapted);
         }
-        st.rows16(low, f, cv, bias, m, r0, adapted);
     }
 }
 
