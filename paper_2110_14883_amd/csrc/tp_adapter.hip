@@ -385,7 +385,7 @@ struct UpStrip {
             }
             if constexpr (DROP) {
                 const uint32_t row = p.drop.row0 + (uint32_t)(t.row0 + r), group = p.drop.group0 + (uint32_t)(n >> 3);
-                const u32x4_t bits = WIDE ? draw(m, group, row) : draw_shared(m, group, group + 8, row);
+                const u32x4_t bits = WIDE ? draw(m, group, row) : draw_shared(m, group, row, group + 8, row);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] += keeps(m, bits, j) ? acc[j][e] : 0.0f;
             } else {

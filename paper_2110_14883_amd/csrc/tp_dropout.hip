@@ -8,40 +8,80 @@ namespace tpl {
 
 namespace {
 
-// Eight columns of a row per thread and a grid that covers the block, streaming hints on everything (as tp_dgelu_kernel).  A dropped element
-// is a zero whatever its input was: it is chosen, not multiplied.
+// Eight columns per thread and a grid that covers the block, streaming hints on everything (as tp_dgelu_kernel).  A dropped element is a zero whatever
+// its input was: it is chosen, not multiplied.
+// With bf16 in and out a thread has the eight columns of a group.  With an fp32 side it has four columns of one group and four of the group 32 further on in
+// the block (neighbouring threads the other halves): every access is then 16 or 8 neighbouring bytes a lane.  (32 bytes a lane
+// in two halves: 16384 x 4096 fp32 to bf16 with residual 86.4 us against 82.3, fp32 to fp32 96.5 / 83.2, bf16 to fp32 with residual 111 / 83.)
 template <bool X_F32, bool GELU, bool PRE, bool Y_F32>
 __global__ __launch_bounds__(256) void tp_dropout_kernel(const DropArgs drop, const void* x, int64_t ldx, const uint16_t* bias, const uint16_t* res,
                                                          int64_t ldr, void* y, int64_t ldy, uint16_t* pre, int64_t ldp, const uint32_t total,
                                                          const Divisor d) {
-    const uint32_t idx = blockIdx.x * 256u + threadIdx.x;
-    if (idx >= total) return;
-    const int64_t r = quotient(d, idx);
-    const uint32_t g = idx - (uint32_t)r * d.d, n = g * 8;
-    float v[8];
-    if constexpr (X_F32) {
-        const f32x4_t* const src = reinterpret_cast<const f32x4_t*>(static_cast<const float*>(x) + r * ldx + n);
-        const f32x4_t a = __builtin_nontemporal_load(src), b = __builtin_nontemporal_load(src + 1);
+    constexpr int N = X_F32 || Y_F32 ? 2 : 1, C = 8 / N;                  // places, columns in each
+    const uint32_t thread = blockIdx.x * 256u + threadIdx.x;
+    const uint32_t first = N == 1 ? thread : (thread & ~63u) + ((thread & 63u) >> 1);
+    if (first >= total) return;                                           // (both threads of a pair)
+    const bool both = N > 1 && first + 32 < total;                        // (else the second place is the first again, and not stored)
+    uint32_t g[N], n[N];
+    int64_t r[N];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-    } else {
-        const u32x4_t a = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(x) + r * ldx + n));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_lo(a[i]); v[2 * i + 1] = bf16_hi(a[i]); }
+    for (int i = 0; i < N; ++i) {
+        const uint32_t idx = i && both ? first + 32 : first;
+        r[i] = quotient(d, idx);
+        g[i] = idx - (uint32_t)r[i] * d.d;
+        n[i] = g[i] * 8 + (N == 1 ? 0 : 4 * (thread & 1));
     }
-    u32x4_t q = {0u, 0u, 0u, 0u}, b = {0u, 0u, 0u, 0u};
-    if (res) q = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(res + r * ldr + n));
-    if (bias) b = *reinterpret_cast<const u32x4_t*>(bias + n);
+    auto load_bf16 = [&](const uint16_t* p, int64_t ld) __attribute__((always_inline)) {
+        if constexpr (N == 1) {
+            return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + r[0] * ld + n[0]));
+        } else {
+            const u32x2_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p + r[0] * ld + n[0]));
+            const u32x2_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p + r[N - 1] * ld + n[N - 1]));
+            return u32x4_t{v[0], v[1], w[0], w[1]};
+        }
+    };
+    auto store_bf16 = [&](uint16_t* p, int64_t ld, const float (&v)[8]) __attribute__((always_inline)) {
+        const u32x4_t o = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        if constexpr (N == 1) {
+            __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t*>(p + r[0] * ld + n[0]));
+        } else {
+            __builtin_nontemporal_store(u32x2_t{o[0], o[1]}, reinterpret_cast<u32x2_t*>(p + r[0] * ld + n[0]));
+            if (both) __builtin_nontemporal_store(u32x2_t{o[2], o[3]}, reinterpret_cast<u32x2_t*>(p + r[N - 1] * ld + n[N - 1]));
+        }
+    };
+    // everything is asked for, then the draw, which needs none of it, then the values
+    f32x4_t xf[N];
+    u32x4_t xb, q = {0u, 0u, 0u, 0u}, b = {0u, 0u, 0u, 0u};
+    if constexpr (X_F32) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) xf[i] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(static_cast<const float*>(x) + r[i] * ldx + n[i]));
+    } else {
+        xb = load_bf16(static_cast<const uint16_t*>(x), ldx);
+    }
+    if (res) q = load_bf16(res, ldr);
+    if (bias) {
+        if constexpr (N == 1) {
+            b = *reinterpret_cast<const u32x4_t*>(bias + n[0]);
+        } else {
+            const u32x2_t v = *reinterpret_cast<const u32x2_t*>(bias + n[0]), w = *reinterpret_cast<const u32x2_t*>(bias + n[N - 1]);
+            b = u32x4_t{v[0], v[1], w[0], w[1]};
+        }
+    }
     const Mask m = open_mask(drop);
-    const u32x4_t bits = draw(m, drop.group0 + g, drop.row0 + (uint32_t)r);
+    const u32x4_t bits = N == 1 ? draw(m, drop.group0 + g[0], drop.row0 + (uint32_t)r[0])
+                                : draw_shared(m, drop.group0 + g[0], drop.row0 + (uint32_t)r[0], drop.group0 + g[N - 1], drop.row0 + (uint32_t)r[N - 1]);
+    __builtin_amdgcn_sched_barrier(0);
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (X_F32) v[j] = xf[j / C][j % C & 3];
+        else                 v[j] = j & 1 ? bf16_hi(xb[j >> 1]) : bf16_lo(xb[j >> 1]);
+    }
     if (bias) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) { v[2 * i] += bf16_lo(b[i]); v[2 * i + 1] += bf16_hi(b[i]); }
     }
-    if constexpr (PRE) {
-        const u32x4_t s = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-        __builtin_nontemporal_store(s, reinterpret_cast<u32x4_t*>(pre + r * ldp + n));
-    }
+    if constexpr (PRE) store_bf16(pre, ldp, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if constexpr (GELU) v[i] = gelu_f(v[i]);
@@ -52,12 +92,13 @@ __global__ __launch_bounds__(256) void tp_dropout_kernel(const DropArgs drop, co
         for (int i = 0; i < 4; ++i) { v[2 * i] += bf16_lo(q[i]); v[2 * i + 1] += bf16_hi(q[i]); }
     }
     if constexpr (Y_F32) {
-        f32x4_t* const to = reinterpret_cast<f32x4_t*>(static_cast<float*>(y) + r * ldy + n);
-        __builtin_nontemporal_store(f32x4_t{v[0], v[1], v[2], v[3]}, to);
-        __builtin_nontemporal_store(f32x4_t{v[4], v[5], v[6], v[7]}, to + 1);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i == 0 || both)
+                __builtin_nontemporal_store(f32x4_t{v[C * i], v[C * i + 1], v[C * i + 2], v[C * i + 3]},
+                                            reinterpret_cast<f32x4_t*>(static_cast<float*>(y) + r[i] * ldy + n[i]));
     } else {
-        const u32x4_t o = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-        __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(y) + r * ldy + n));
+        store_bf16(static_cast<uint16_t*>(y), ldy, v);
     }
 }
 
@@ -84,8 +125,10 @@ __global__ __launch_bounds__(256) void tp_dropout_bwd_kernel(const DropArgs drop
     u32x4_t a = {0u, 0u, 0u, 0u};
     if constexpr (GELU) a = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(pre + r * ld_pre + n));
     const Mask m = open_mask(drop);
+    const u32x4_t bits = draw(m, drop.group0 + g, drop.row0 + (uint32_t)r);      // (while the loads are under way)
+    __builtin_amdgcn_sched_barrier(0);
     float v[8];
-    slope8<GELU>(m, drop.factor, draw(m, drop.group0 + g, drop.row0 + (uint32_t)r), s, a, v);
+    slope8<GELU>(m, drop.factor, bits, s, a, v);
     const u32x4_t o = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t*>(dx + r * ld_dx + n));
 }
@@ -106,7 +149,7 @@ __global__ __launch_bounds__(COLS * 4) void tp_dropout_bwd_sum_kernel(const Drop
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (c < cols) {
         for (int64_t r0 = begin + rl; r0 < end; r0 += 4 * LANES) {
-            u32x4_t g[4], a[4];
+            u32x4_t g[4], a[4], bits[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {                        // (rows past the end: the last one again, dropped below)
                 const int64_t r = r0 + LANES * u < end ? r0 + LANES * u : end - 1;
@@ -115,11 +158,14 @@ __global__ __launch_bounds__(COLS * 4) void tp_dropout_bwd_sum_kernel(const Drop
                 else                a[u] = g[u];
             }
 #pragma unroll
+            for (int u = 0; u < 4; ++u) bits[u] = draw(m, drop.group0 + (uint32_t)(c >> 3), drop.row0 + (uint32_t)(r0 + LANES * u));   // (while the loads are under way)
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int64_t r = r0 + LANES * u;
                 if (r >= end) break;
                 float v[8];
-                slope8<GELU>(m, drop.factor, draw(m, drop.group0 + (uint32_t)(c >> 3), drop.row0 + (uint32_t)r), g[u], a[u], v);
+                slope8<GELU>(m, drop.factor, bits[u], g[u], a[u], v);
                 const u32x4_t o = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
                 __builtin_nontemporal_store(o, reinterpret_cast<u32x4_t*>(dx + r * ld_dx + c));
 #pragma unroll

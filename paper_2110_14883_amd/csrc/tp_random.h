@@ -36,12 +36,12 @@ __device__ __forceinline__ u32x4_t draw(const Mask& m, uint32_t group, uint32_t 
     }
     return u32x4_t{x0, x1, x2, x3};
 }
-// The same for a lane that holds columns 4 i .. 4 i + 3 of two stretches of columns, i = its number, `group0` and `group1` the groups of those (lanes
-// 2 j and 2 j + 1 share both): the even lane draws one, the odd one the other, and they hand each other the half that is its neighbour's.
-// Words 0, 1 are the bits of the first four columns, 2, 3 of the others.
-__device__ __forceinline__ u32x4_t draw_shared(const Mask& m, uint32_t group0, uint32_t group1, uint32_t row) {
+// The same for a lane that holds four neighbouring columns in two places, lanes 2 j and 2 j + 1 the halves of one group in each: the even lane draws for
+// the first place, the odd one for the second, and they hand each other the half that is its neighbour's.  Words 0, 1 are the bits of the
+// first place's columns, 2, 3 of the second's.
+__device__ __forceinline__ u32x4_t draw_shared(const Mask& m, uint32_t group0, uint32_t row0, uint32_t group1, uint32_t row1) {
     const bool odd = threadIdx.x & 1;
-    const u32x4_t w = draw(m, odd ? group1 : group0, row);
+    const u32x4_t w = draw(m, odd ? group1 : group0, odd ? row1 : row0);
     const int a = odd ? w[0] : w[2], b = odd ? w[1] : w[3];
     const uint32_t x = (uint32_t)__builtin_amdgcn_mov_dpp(a, 0xB1, 0xF, 0xF, true), y = (uint32_t)__builtin_amdgcn_mov_dpp(b, 0xB1, 0xF, 0xF, true);   // lanes 1 0 3 2
     return u32x4_t{odd ? x : w[0], odd ? y : w[1], odd ? w[2] : x, odd ? w[3] : y};
