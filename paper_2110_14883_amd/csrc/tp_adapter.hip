@@ -119,9 +119,10 @@ __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, cons
 // direct-to-LDS loads of 8 whole lines each, with no barrier in the loop.  (Fragments loaded straight into registers, 64 bytes of 16 rows an
 // instruction: 16384 x 4096, 16 ranks 34.2 us against XXX.)
 // ---------------------------------------------------------------------------------------------
-constexpr int down_waves(int mt, int rb) { return mt + rb <= 5 ? 8 : 4; }
-template <int MT, int RB> struct DownShape {
-    static constexpr int WAVES = down_waves(MT, RB);
+// (with a mask to draw, the waves count for more than the slots)
+constexpr int down_waves(int mt, int rb, bool drop) { return mt + rb <= (drop ? 8 : 5) ? 8 : 4; }
+template <int MT, int RB, bool DROP> struct DownShape {
+    static constexpr int WAVES = down_waves(MT, RB, DROP);
     static constexpr int SLOT = (MT + RB) * 2048;                                               // a unit: lines of 16 MT rows, of 16 RB ranks
     static constexpr int FIT = 163840 / (WAVES * SLOT), NS = FIT > 4 ? 4 : FIT;
     static constexpr int PART = 16 * RB + 4, SUMS = WAVES * 16 * PART * 4;                      // the waves' sums of 16 rows
@@ -188,6 +189,15 @@ __device__ __forceinline__ void down_sums(const DownArgs& p, const Tile& t, cons
     for (int u = share; u < total; u += shares) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");               // the slot to refill has been read
         fetch(slot == 0 ? NS - 1 : slot - 1);
+        u32x4_t bits[DROP ? 2 * MT : 1];
+        if constexpr (DROP) {                                            // (the draws need nothing that is under way)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    bits[MT * h + i] = draw(m, p.group0[step] + 8 * kt + 4 * h + g, p.drop.row0 + (uint32_t)(t.row0 + 16 * i + c));
+            __builtin_amdgcn_sched_barrier(0);
+        }
         wait_vm<(NS - 1) * LOADS>();
         asm volatile("" ::: "memory");
         const uint32_t at = mine + (uint32_t)(slot * SLOT);
@@ -203,8 +213,7 @@ __device__ __forceinline__ void down_sums(const DownArgs& p, const Tile& t, cons
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 u32x4_t x = __builtin_bit_cast(u32x4_t, frag(at, i));
-                if constexpr (DROP)
-                    x = clear_dropped(m, draw(m, p.group0[step] + 8 * kt + 4 * h + g, p.drop.row0 + (uint32_t)(t.row0 + 16 * i + c)), x);
+                if constexpr (DROP) x = clear_dropped(m, bits[MT * h + i], x);
 #pragma unroll
                 for (int j = 0; j < RB; ++j) acc[i][j] = mfma(__builtin_bit_cast(u32x4_t, f[j]), x, acc[i][j]);
             }
@@ -223,8 +232,8 @@ __device__ __forceinline__ f32x4_t waves_sum(const float* part, int row, int q) 
     return s;
 }
 template <int MT, int RB, bool DROP>
-__global__ __launch_bounds__(64 * down_waves(MT, RB)) void tp_adapter_down_kernel(const DownArgs p) {
-    using Sh = DownShape<MT, RB>;
+__global__ __launch_bounds__(64 * down_waves(MT, RB, DROP)) void tp_adapter_down_kernel(const DownArgs p) {
+    using Sh = DownShape<MT, RB, DROP>;
     constexpr int WAVES = Sh::WAVES;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     preload(p);
@@ -618,26 +627,34 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
         u32x4_t rows[8], r[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) rows[j] = buf_load16(rr, in ? (uint32_t)(((8 * g + j) * q.ldr + n) * 2) : OOB_OFFSET);
+        uint32_t first[RB][8];
+        auto plane = [&](int z, int i, int j) __attribute__((always_inline)) {
+            const __amdgpu_buffer_rsrc_t rl = make_rsrc(q.l + z * q.plane + (int64_t)row * p.rank, (int64_t)have * p.rank * 4);
+            const int k = rank0 + 16 * i + c;
+            return __builtin_amdgcn_raw_buffer_load_b32(rl, k < p.rank ? ((8 * g + j) * p.rank + k) * 4 : (int)OOB_OFFSET, 0, 0);
+        };
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) first[i][j] = plane(0, i, j);
+        if (q.dropped) {                                         // (the draws need nothing that is under way)
+            u32x4_t bits[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) bits[j] = draw(m, p.drop.group0 + (uint32_t)(n >> 3), p.drop.row0 + (uint32_t)(row + 8 * g + j));
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) rows[j] = clear_dropped(m, bits[j], rows[j]);
+        }
         float v[RB][8];
 #pragma unroll
         for (int i = 0; i < RB; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
-        for (int z = 0; z < q.splits; ++z) {
-            const __amdgpu_buffer_rsrc_t rl = make_rsrc(q.l + z * q.plane + (int64_t)row * p.rank, (int64_t)have * p.rank * 4);
+            for (int j = 0; j < 8; ++j) v[i][j] = as_float(first[i][j]);
+        for (int z = 1; z < q.splits; ++z)
 #pragma unroll
             for (int i = 0; i < RB; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int k = rank0 + 16 * i + c;
-                    v[i][j] += __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rl, k < p.rank ? ((8 * g + j) * p.rank + k) * 4 : (int)OOB_OFFSET, 0, 0));
-                }
-        }
-        if (q.dropped) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                rows[j] = clear_dropped(m, draw(m, p.drop.group0 + (uint32_t)(n >> 3), p.drop.row0 + (uint32_t)(row + 8 * g + j)), rows[j]);
-        }
+                for (int j = 0; j < 8; ++j) v[i][j] += as_float(plane(z, i, j));
         transpose8(rows, r);
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
@@ -736,7 +753,7 @@ hipError_t allow_lds(K kernel, int bytes, std::atomic<uint64_t>& done) {
 }
 template <int MT, int RB, bool DROP>
 hipError_t down_as(const DownArgs& a, hipStream_t s) {
-    using Sh = DownShape<MT, RB>;
+    using Sh = DownShape<MT, RB, DROP>;
     static std::atomic<uint64_t> done{0};
     if (hipError_t e = allow_lds(tp_adapter_down_kernel<MT, RB, DROP>, Sh::BYTES, done); e != hipSuccess) return e;
     return launch_kernel(tp_adapter_down_kernel<MT, RB, DROP>, dim3((unsigned)a.tiles, (unsigned)a.splits), dim3(64 * Sh::WAVES), Sh::BYTES, s, a);
