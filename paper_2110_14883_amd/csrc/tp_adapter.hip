@@ -765,8 +765,7 @@ hipError_t down_rank(const DownArgs& a, hipStream_t s) {
     if (a.rank <= 16) return down<MT, 1>(a, s);
     if (a.rank <= 32) return down<MT, 2>(a, s);
     if (a.rank <= 64) return down<MT, 4>(a, s);
-    if constexpr (MT <= 2) return down<MT, 8>(a, s);
-    return hipErrorInvalidValue;
+    return down<MT, 8>(a, s);
 }
 
 template <int GP, int TERMS>

@@ -87,7 +87,7 @@ Split plan_products(int64_t rows, int64_t segments, int64_t k, int n_steps, int6
     s.tile = 16;
     s.up_tile = 16;
     if (!brief) {
-        s.tile = rank > 64 || tiles(64) <= 128 || rounds(tiles(32)) * (32 + 8) < rounds(tiles(64)) * (64 + 8) ? 32 : 64;
+        s.tile = tiles(64) <= 128 || rounds(tiles(32)) * (32 + 8) < rounds(tiles(64)) * (64 + 8) ? 32 : 64;
         int64_t best = INT64_MAX;
         const int strips = (int)((up_cols + 127) / 128);
         for (int tile : {64, 128, 32}) {
