@@ -381,7 +381,8 @@ typedef struct { void* ptr; int64_t ld, stride; } tp_factor_out_t;
  * columns of A, the reduction that completes c completes it, and epi, preact and a bf16 y are refused as in tp_linear_fwd.
  * Defined by: the adapted layer X (W + s A^T B) under the partition of tp_linear_fwd (Section 2.2): A is cut like W's rows, B like W's columns.
  * V is fp32; in the second product it stands as a sum of bf16 terms that is off by 2^-17 (bf16 y) or 2^-25 (fp32 y) of it.
- * Errors: TP_ERR_NULL, TP_ERR_MODE, TP_ERR_GRID, TP_ERR_SHAPE (also: rank, pool or segment counts out of range), TP_ERR_ALIGN, TP_ERR_DTYPE,
+ * Errors: TP_ERR_NULL, TP_ERR_MODE, TP_ERR_GRID, TP_ERR_SHAPE (also: rank, pool or segment counts out of range, or more than 2^22 tiles of 16 rows of
+ * short segments or 64 of long ones), TP_ERR_ALIGN, TP_ERR_DTYPE,
  * TP_ERR_WORKSPACE, TP_ERR_HIP; nothing is launched unless every check has passed.
  */
 int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, const tp_adapters_t* adapters, const tp_cblk_t* x_blocks,

@@ -820,8 +820,7 @@ hipError_t launch_up(const UpArgs& a, hipStream_t s) {
 hipError_t launch_grad(const GradArgs& a, hipStream_t s) {
     const int strips0 = (a.side[0].cols + 127) / 128, strips = strips0 + (a.sides > 1 ? (a.side[1].cols + 127) / 128 : 0);
     const int rb = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4, chunks = (a.rank + 16 * rb - 1) / (16 * rb);
-    const int64_t blocks = (int64_t)strips * chunks * a.shares * a.seg.pool;
-    if (blocks > INT32_MAX || a.seg.pool > 32767) return hipErrorInvalidValue;
+    const int64_t blocks = (int64_t)strips * chunks * a.shares * a.seg.pool;      // (the caller has looked at how many)
     if (hipError_t e = launch_kernel(rb == 1 ? tp_adapter_grad_kernel<1> : rb == 2 ? tp_adapter_grad_kernel<2> : tp_adapter_grad_kernel<4>,
                                      dim3((unsigned)blocks), dim3(64 * GRAD_WAVES), 0, s, a, strips0, strips); e != hipSuccess || a.shares == 1)
         return e;

@@ -103,11 +103,16 @@ Split plan_products(int64_t rows, int64_t segments, int64_t k, int n_steps, int6
     s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / s.tiles, units / 8, 16}));
     return s;
 }
+// A launch's threads are counted in 32 bits: at most 2^22 tiles, and 2^23 workgroups of the gradients
+constexpr int64_t kMostTiles = (int64_t)1 << 22, kMostGradBlocks = (int64_t)1 << 23;
+int check_tiles(const Split& s) { return s.tiles > kMostTiles || s.up_tiles > kMostTiles ? TP_ERR_SHAPE : TP_OK; }
+
 // Elements of a factor up to which both products of a short segment go into one launch, where every workgroup of a tile reads it whole
 constexpr int64_t kFewFactor = (int64_t)1 << 20;
 // Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) for two a CU (four: 63 us for 55, and more planes), 128 rows a share at least
+int64_t grad_blocks(int64_t cols, int pool, int rank) { return (cols + 127) / 128 * ((rank + 63) / 64) * pool; }
 int plan_grad(int64_t rows, int64_t cols, int pool, int rank) {
-    const int64_t blocks = (cols + 127) / 128 * ((rank + 63) / 64) * pool;
+    const int64_t blocks = grad_blocks(cols, pool, rank);
     return (int)std::max<int64_t>(1, std::min<int64_t>({(512 + blocks - 1) / blocks, rows / 128, 32}));
 }
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -182,6 +187,7 @@ int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
         if (y.ptr && y.dtype != TP_F32) return TP_ERR_DTYPE;
     }
     const Split sp = plan_products(s.m, adapters->n_segments, s.k, s.n_steps, s.n, adapters->rank);
+    if (int e = check_tiles(sp)) return e;
     const Space need = space_fwd(s, adapters);
     float* const planes = v && sp.splits == 1 ? v : static_cast<float*>(workspace);
     DownArgs d{};
@@ -225,6 +231,8 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
     if (!aligned16(v)) return TP_ERR_ALIGN;
     if (dx.ptr && x.partial && dx.dtype != TP_F32) return TP_ERR_DTYPE;
     const Split sp = plan_products(x.m, adapters->n_segments, x.k, x.n_steps, x.n, adapters->rank);
+    if (int e = check_tiles(sp)) return e;
+    if (grad_blocks(x.n + f.n, adapters->n_adapters, adapters->rank) > kMostGradBlocks) return TP_ERR_SHAPE;
     const Space need = space_bwd(f, x, adapters);
     char* at = static_cast<char*>(workspace);
     float* const planes = reinterpret_cast<float*>(at);

@@ -64,6 +64,9 @@ def test_refusals_forward():
     f = dict(grid=row, dims=(32, 128, 128))
     assert _fwd(y=Y, **f) == 6 and _fwd(y=(0x80000, 128, 1), epi=T.EPI_BIAS, bias=0x100, **f) == 2 and _fwd(y=(0x80000, 128, 1), pre=(0xC0000, 128, 0), **f) == 2
     assert _fwd(ad=ad(n_segments=0)) == 0                # nothing to do
+    # more tiles than a launch has threads for
+    many = dict(dims=(1 << 23, 64, 128), ws=(0x1000000, 1 << 50), c=(0x4000000000, 128, 0), y=(0x8000000000, 128, 0))
+    assert _fwd(ad=ad(n_segments=1 << 23), **many) == 4
 
 
 def test_refusals_backward():
@@ -73,6 +76,8 @@ def test_refusals_backward():
     assert _bwd(da=(0x90000, 64, 1000)) == 4 and _bwd(da=(0x90000, 60, 1024)) == 5 and _bwd(db=(0xB0004, 128, 2048)) == 5 and _bwd(v=0xA0004) == 5
     assert _bwd(dx=(0x40020, 64, 0)) == 4 and _bwd(dx=(0x80000, 64, 7)) == 6 and _bwd(ws=None) == 7 and _bwd(drop=T.Dropout(float("nan"), 1)) == 2
     assert _bwd(grid=T.Grid(T.MODE_1D_COL, p=2), dims=(32, 64, 256)) == 6          # a partial dX in bf16
+    assert _bwd(ad=ad(n_adapters=32767, n_segments=1 << 20), dims=(32, 1 << 18, 1 << 18), dy=[(0x10000, 1 << 18)], bs=[(0x10000, 1 << 18, 1 << 22)],
+                own=(0x10000, 1 << 18)) == 4             # more workgroups than a launch has threads for
     none = dict(dx=None, da=None, db=None)
     assert _bwd(dy=None, bs=None, a=None, base=None, x=None, own=None, v=None, ws=None, **none) == 0
 
@@ -284,6 +289,55 @@ def test_ranks_and_segments(rank, kind):
 @pytest.mark.parametrize("rank,kind,p", [(16, "one", 0.0), (8, "gaps and empties", 0.3), (64, "one", 0.5)])
 def test_extents(m, h, f, rank, kind, p):
     run_case(T.Grid(T.MODE_1D_COL), (m, h, f), rank, kind, p=p, seed=2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,h,f,rank,kind,p", [
+    (130, 64, 5000, 16, "single rows", 0.0), (70, 4096, 4104, 48, "single rows", 0.0),       # many strips a wave in one launch
+    (3, 16384, 2056, 128, "one", 0.0), (40, 9000, 264, 128, "single rows", 0.0),             # factors too large for that
+    (40, 136, 264, 16, "single rows", 0.4),                                                  # and dropout
+    (9000, 136, 1288, 16, "many", 0.2), (9000, 136, 640, 64, "gaps and empties", 0.0), (5000, 72, 1160, 128, "many", 0.0), (20000, 328, 520, 8, "one", 0.1),
+    (1300, 40, 4104, 32, "gaps and empties", 0.3)])
+def test_every_plan(m, h, f, rank, kind, p):
+    run_case(T.Grid(T.MODE_1D_COL), (m, h, f), rank, kind, y_type=F32 if rank % 16 else BF, p=p, seed=15)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("q,h,p", [(9, 40, 0.0), (9, 72, 0.3), (16, 8, 0.0)])
+def test_many_short_steps(q, h, p):
+    """More steps than waves, fewer units than waves, units that end inside a step."""
+    run_case(T.Grid(T.MODE_2D, q=q, ri=1, rj=q - 1), (q * 37, q * h, q * 48), 16, "gaps and empties", p=p, seed=16)
+    run_case(T.Grid(T.MODE_2D, q=q, ri=1, rj=q - 1), (q * 37, q * h, q * 48), 72, "single rows", p=p, seed=17)
+
+
+@pytest.mark.gpu
+def test_no_segments_and_everything_dropped():
+    m, h, n, rank = 50, 72, 136, 16
+    g = _g(18)
+    grid, dims = T.Grid(T.MODE_1D_COL), (m, h, n)
+    x, a, b, c, dy = (t.contiguous() for t in (_strided(g, m, h), _strided(g, 2, rank, h), _strided(g, 2, rank, n), _strided(g, m, n), _strided(g, m, n)))
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+
+    def both(ad, drop, x):
+        y, v, dx = torch.full((m, n), 7.0, dtype=BF, device="cuda"), torch.full((m, rank), 7.0, device="cuda"), torch.full((m, h), 7.0, dtype=BF, device="cuda")
+        da, db = torch.full((2, rank, h), 7.0, device="cuda"), torch.full((2, rank, n), 7.0, device="cuda")
+        T.tp_adapter_fwd(grid, dims, 1, ad, [x], [a], b, c, None, 0, y, v=v, dropout=drop, workspace=ws)
+        T.tp_adapter_bwd(grid, dims, 1, ad, [dy], [b], a=a, dx_base=c[:, :h], dx=dx, x_own=x, da=da, dy_own=dy, v=v, db=db, dropout=drop, workspace=ws)
+        return y, v, dx, da, db
+
+    for ad in (T.Adapters(i32([0]), i32([]), 2, rank), T.Adapters(i32([0, 0, 0]), i32([0, 1]), 2, rank)):
+        y, v, dx, da, db = both(ad, None, x)
+        assert (y == 7).all() and (v == 7).all() and (dx == 7).all() and (da == 0).all() and (db == 0).all()
+    y, v, dx, da, db = both(T.Adapters(i32([0, m]), i32([1]), 2, rank), T.Dropout(1.0, 3), x * float("nan"))
+    assert torch.equal(y, c) and (v == 0).all() and torch.equal(dx, c[:, :h]) and (da == 0).all() and (db == 0).all()
+    # NaN and infinities where the mask drops them
+    drop, ad = T.Dropout(0.5, 4, 5), T.Adapters(i32([0, 20, m]), i32([1, 0]), 2, rank)
+    keep = torch.from_numpy(keep_mask((0.5, 4, 5, 0, 0), m, h)).cuda()
+    clean = torch.where(keep, x, torch.zeros_like(x))
+    dirty = torch.where(keep, x, torch.tensor([float("nan"), float("inf")], device="cuda").repeat(h // 2).to(BF))
+    for s, t in zip(both(ad, drop, clean), both(ad, drop, dirty)):
+        assert torch.equal(s, t) and torch.isfinite(t).all()
 
 
 @pytest.mark.gpu
