@@ -531,21 +531,23 @@ __global__ __launch_bounds__(64 * few_waves(RB)) void tp_adapter_few_kernel(cons
     const int strips = (p.cols + 127) / 128, step = gridDim.y * Sh::WAVES;
     int strip = blockIdx.y * Sh::WAVES + w;
     constexpr int EARLY = RB <= 2 ? 2 : 1;                               // strips whose factor comes in early
-    u32x4_t f[EARLY][UpShape<GP, TERMS>::NS][8];
-    CRows<C32> cv;
+    u32x4_t f[EARLY][UpShape<GP, TERMS>::NS][8], bias[EARLY];
+    CRows<C32> cv[EARLY];
     char* const low = lds + Sh::SUMS;
-    if (adapted) {
 #pragma unroll
-        for (int s = 0; s < EARLY; ++s)
-            if (strip + s * step < strips) Strip(p, t, strip + s * step).load_factor(f[s]);
-    }
+    for (int s = 0; s < EARLY; ++s)
+        if (strip + s * step < strips) {
+            const Strip st(p, t, strip + s * step);
+            if (adapted) st.load_factor(f[s]);
+            st.load_c(cv[s], 0);
+            bias[s] = st.load_bias();
+        }
     if (adapted) {
         const float scale = p.scale ? p.scale[t.id] : 1.0f;
         f32x4_t acc[1][RB];
         const uint32_t ring = (uint32_t)(w * Sh::NS * Sh::SLOT);
         if (t.rows <= 8) down_sums<1, RB, Sh::NS, false, 1>(d, t, w, Sh::WAVES, ring, acc);
         else             down_sums<1, RB, Sh::NS, false, 2>(d, t, w, Sh::WAVES, ring, acc);
-        if (strip < strips) Strip(p, t, strip).load_c(cv, 0);
         __syncthreads();
         float* const part = reinterpret_cast<float*>(lds);
 #pragma unroll
@@ -569,16 +571,15 @@ __global__ __launch_bounds__(64 * few_waves(RB)) void tp_adapter_few_kernel(cons
     for (int s = 0; s < EARLY; ++s, strip += step) {
         if (strip >= strips) return;
         const Strip st(p, t, strip);
-        if (s || !adapted) st.load_c(cv, 0);
         if (adapted) st.turn(f[s]);
-        st.rows16(low, f[s], cv, st.load_bias(), none, 0, adapted);
+        st.rows16(low, f[s], cv[s], bias[s], none, 0, adapted);
     }
     for (; strip < strips; strip += step) {
         const Strip st(p, t, strip);
         if (adapted) st.load_factor(f[0]);
-        st.load_c(cv, 0);
+        st.load_c(cv[0], 0);
         if (adapted) st.turn(f[0]);
-        st.rows16(low, f[0], cv, st.load_bias(), none, 0, adapted);
+        st.rows16(low, f[0], cv[0], st.load_bias(), none, 0, adapted);
     }
 }
 
