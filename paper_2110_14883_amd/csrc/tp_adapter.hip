@@ -317,15 +317,16 @@ struct UpStrip {
             }
         }
     }
-    // the strip of the factor, and its rows turned into matrix operands
+    // the strip of the factor, and its rows turned into matrix operands.  Up to 16 ranks both halves of the wave need the same eight rows a lane: each
+    // loads four of them, and they swap.
     __device__ __forceinline__ void load_factor(u32x4_t (&f)[Sh::NS][8]) const {
         const __amdgpu_buffer_rsrc_t rf = make_rsrc(static_cast<const uint16_t*>(p.f) + t.id * p.stride, ((int64_t)(p.rank - 1) * p.ldf + p.cols) * 2);
 #pragma unroll
         for (int s = 0; s < Sh::NS; ++s) {
-            const int k = 8 * (GP >= 4 ? 4 * s + g : g & (GP - 1));
+            const int k = GP >= 4 ? 8 * (4 * s + g) : 8 * (g & 1) + 4 * (g >> 1);
             const bool ok = k < p.rank;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < (GP >= 4 ? 8 : 4); ++j) {
                 const uint32_t at = (uint32_t)(((k + j) * p.ldf + n) * 2);
                 if constexpr (WIDE) {
                     f[s][j] = buf_load16(rf, ok && in ? at : OOB_OFFSET);
@@ -338,6 +339,16 @@ struct UpStrip {
         }
     }
     __device__ __forceinline__ void turn(u32x4_t (&f)[Sh::NS][8]) const {
+        if constexpr (GP < 4) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {                            // lanes 0 - 31 of both, lanes 32 - 63 of both
+                    const u32x2_t x = __builtin_amdgcn_permlane32_swap(f[0][j][i], f[0][j][i], false, false);
+                    f[0][j][i] = x[0];
+                    f[0][4 + j][i] = x[1];
+                }
+        }
 #pragma unroll
         for (int s = 0; s < Sh::NS; ++s) {
             u32x4_t o[8];
