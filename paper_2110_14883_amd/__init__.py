@@ -1,5 +1,5 @@
-"""MI355X-native per-rank tensor-parallel linear layer (1D / 2D-SUMMA / 2.5D / 3D): a thin
-binding over libtplinear.so.  Importing this package does not load the library; the first call
+"""MI355X-native per-rank tensor-parallel linear layer (1D / 2D-SUMMA / 2.5D / 3D), with dropout and
+low-rank adapters beside it: a thin binding over libtplinear.so.  Importing this package does not load the library; the first call
 does, and fails loudly if it has not been built (python -m paper_2110_14883_amd.build)."""
 from .binding import (  # noqa: F401
     EPI_BIAS, EPI_BIAS_GELU, EPI_NONE, MODE_1D_COL, MODE_1D_ROW, MODE_2D, MODE_2P5D, MODE_3D, MODE_3D_GATHERED,

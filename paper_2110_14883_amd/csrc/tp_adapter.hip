@@ -3,12 +3,15 @@
 //   forward   V = drop(X) A_i^T,   Y = act(C + s_i V B_i + bias)
 //   backward  U = dY B_i^T,        dX = dX_base + drop'(s_i U A_i),    dA_i = s_i U^T drop(X),   dB_i = s_i V^T dY
 // Both factors lie as `rank` long rows, so forward and backward are the same three products:
-//   down  [rows, K] x [rank, K]^T      both operands contraction-contiguous: fragments straight from memory
+//   down  [rows, K] x [rank, K]^T      both operands contraction-contiguous, through LDS
 //   up    [rows, rank] x [rank, cols]  the factor's 8 x 8 blocks transposed in registers
-//   grad  [rows, rank]^T x [rows, cols]
+//   grad  [rows, rank]^T x [rows, cols]  the same turn of the second operand, sums over rows
 // All three are bound by memory: the rank is at most 128, so a row of X or Y that is read takes 2 to 64 flops a byte.  V and U stay in fp32.  Where they
 // are a matrix operand they go in as a sum of bf16 terms, two (2^-17) for bf16 results and three (2^-25) for fp32 ones: the matrix
 // unit has the time, and rounding them once would cost a bf16 step of the adapters' part.
+// Measured (all of a call, us, and the bytes it cannot do without over that): one token of 4096 x 4096, 16 ranks 7.3; 96 tokens over 48 adapters 10.0; 5923
+// rows in 12 segments, 32 ranks, GeLU 56 (4.4 TB/s); 2048 x 4 x 2048 x 8192, 64 ranks, dropout 30 (3.5); backward of 16384 x 4096 x 4096, 16 ranks, dropout,
+// fp32 176 (4.6), of 32896 x 640 over 2 x 2560, 8 ranks 106 (4.4).  A large copy reaches 5.2 TB/s.
 //
 // Rows come in segments, a request each, described by device arrays.  A workgroup works on a tile of one segment's rows: it finds its tile from
 // the offsets itself (one trip to memory for up to 64 segments), so a call is the same launches whatever the lengths, and can be captured.  Offsets are
@@ -117,7 +120,7 @@ __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, cons
 // down.  A tile of 16 MT rows by all 16 RB ranks.  The waves of a workgroup, and the workgroups of a tile, take the units of 64 k in turn (so neighbouring
 // waves read neighbouring cache lines of a row), and the waves' sums meet in LDS in their order.  A wave has a ring of LDS slots of its own, filled by
 // direct-to-LDS loads of 8 whole lines each, with no barrier in the loop.  (Fragments loaded straight into registers, 64 bytes of 16 rows an
-// instruction: 16384 x 4096, 16 ranks 34.2 us against XXX.)
+// instruction, kept the address path busy longer: 16384 x 4096, 16 ranks 34.2 us against 28.5, 32896 x 2 x 2560 in 24 segments 67 / 46.)
 // ---------------------------------------------------------------------------------------------
 // (with a mask to draw, the waves count for more than the slots)
 constexpr int down_waves(int mt, int rb, bool drop) { return mt + rb <= (drop ? 8 : 5) ? 8 : 4; }
@@ -521,14 +524,18 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
 // ---------------------------------------------------------------------------------------------
 constexpr int few_waves(int rb) { return rb <= 4 ? 8 : 4; }              // (as many as leave a wave its registers)
 template <int RB> struct FewShape {                                      // RB: blocks of 16 ranks
-    static constexpr int WAVES = few_waves(RB), SLOT = (1 + RB) * 2048, FIT = 163840 / (WAVES * SLOT), NS = FIT > 4 ? 4 : FIT;
+    static constexpr int WAVES = few_waves(RB), SLOT = (1 + RB) * 2048, FIT = 163840 / (WAVES * SLOT);
+    static constexpr int NS = RB == 1 ? 2 : FIT > 4 ? 4 : FIT;           // (up to 16 ranks two workgroups share a CU)
     static constexpr int PART = 16 * RB + 4, SUMS = WAVES * 16 * PART * 4;
     static constexpr int LOW = 16 * UpShape<2 * RB, 3>::ROW;             // behind the waves' sums, where the ring was
     static constexpr int BYTES = WAVES * NS * SLOT > SUMS + LOW ? WAVES * NS * SLOT : SUMS + LOW;
     static_assert(NS >= 1 && BYTES <= 163840);
 };
+// Up to 16 ranks and bf16 throughout the registers are held to what lets two workgroups share a CU (1000 single rows of 4096 x 4096 50 -> 35 us, one row 6.7 -> 6.5);
+// elsewhere that would spill (32 ranks, 1000 rows 57 -> 63).
+constexpr int few_waves_a_simd(int rb, int terms, bool c32) { return rb == 1 && terms == 2 && !c32 ? 4 : 1; }
 template <int RB, int TERMS, bool C32>
-__global__ __launch_bounds__(64 * few_waves(RB)) void tp_adapter_few_kernel(const DownArgs d, const UpArgs p) {
+__global__ __launch_bounds__(64 * few_waves(RB), few_waves_a_simd(RB, TERMS, C32)) void tp_adapter_few_kernel(const DownArgs d, const UpArgs p) {
     constexpr int GP = 2 * RB;
     using Sh = FewShape<RB>;
     using Strip = UpStrip<GP, TERMS, false, C32>;
@@ -541,7 +548,7 @@ __global__ __launch_bounds__(64 * few_waves(RB)) void tp_adapter_few_kernel(cons
     const bool adapted = t.id >= 0;
     const int strips = (p.cols + 127) / 128, step = gridDim.y * Sh::WAVES;
     int strip = blockIdx.y * Sh::WAVES + w;
-    constexpr int EARLY = RB <= 2 ? 2 : 1;                               // strips whose factor comes in early
+    constexpr int EARLY = RB == 2 ? 2 : 1;                               // strips whose factor and C come in early
     u32x4_t f[EARLY][UpShape<GP, TERMS>::NS][8], bias[EARLY];
     CRows<C32> cv[EARLY];
     char* const low = lds + Sh::SUMS;
@@ -606,7 +613,7 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
     const int l = threadIdx.x & 63, c = l & 15, g = l >> 4, w = uni(threadIdx.x >> 6);
     const int chunks = (p.rank + 16 * RB - 1) / (16 * RB);
     // (the shares side by side: an XCD then has its own shares of the rows, and a CU strips of both pairs, of which one may draw a mask: 16384 rows of
-    // 4096 and 4096 columns with dropout 58 us with the strips side by side, XXX so)
+    // 4096 and 4096 columns with dropout 52.2 us, 56.6 with the strips side by side)
     int x = blockIdx.x;
     const int share = x % p.shares; x /= p.shares;
     const int strip_all = x % strips; x /= strips;

@@ -107,8 +107,15 @@ Split plan_products(int64_t rows, int64_t segments, int64_t k, int n_steps, int6
 constexpr int64_t kMostTiles = (int64_t)1 << 22, kMostGradBlocks = (int64_t)1 << 23;
 int check_tiles(const Split& s) { return s.tiles > kMostTiles || s.up_tiles > kMostTiles ? TP_ERR_SHAPE : TP_OK; }
 
-// Elements of a factor up to which both products of a short segment go into one launch, where every workgroup of a tile reads it whole
-constexpr int64_t kFewFactor = (int64_t)1 << 20;
+// Whether both products of short segments go into one launch, where every workgroup of a tile reads the factor A whole: by the elements it has.  GPU time in
+// us, one launch / two, 4096 columns: one row, 16 ranks x 4096 6.7 / 8.3, x 16384 11.7 / 9.9; 96 single rows, 64 ranks x 4096 15.6 / 17.5, x 8192 20.7 / 20.9,
+// x 16384 30.9 / 26.9; 256 single rows, 64 x 16384 35 / 47, 128 x 16384 96 / 97; 1000 single rows, 16 x 4096 50 / 83, 128 x 16384 323 / 330; segments
+// of six rows, 16 of them, 16 x 4096 8.0 / 9.4, 64 x 4096 14.1 / 11.7; 50 of twelve rows, 16 x 1024 8.7 / 9.7, 16 x 4096 11.7 / 10.6.
+bool in_one_launch(const Split& s, int64_t rows, int64_t segments, int64_t factor) {
+    if (s.tile != 16) return false;
+    const int64_t most = s.tiles >= 192 ? 1 << 21 : s.tiles >= 80 ? 1 << 19 : 1 << 17;
+    return factor <= (rows > 8 * segments ? most / 4 : most);
+}
 // Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) for two a CU (four: 63 us for 55, and more planes), 128 rows a share at least
 int64_t grad_blocks(int64_t cols, int pool, int rank) { return (cols + 127) / 128 * ((rank + 63) / 64) * pool; }
 int plan_grad(int64_t rows, int64_t cols, int pool, int rank) {
@@ -205,7 +212,7 @@ int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
         if (int e = check_oblk(preact, s.n, false)) return e;
         if (preact.dtype != TP_BF16) return TP_ERR_DTYPE;
     }
-    const bool few = sp.tile == 16 && !drop && (int64_t)n_steps * s.k * adapters->rank <= kFewFactor;
+    const bool few = !drop && in_one_launch(sp, s.m, adapters->n_segments, n_steps * s.k * adapters->rank);
     u.v = planes; u.v_out = planes == v && !few ? nullptr : v;
     u.bias = epi == TP_EPI_NONE ? nullptr : bias; u.gelu = epi == TP_EPI_BIAS_GELU;
     u.pre = preact.ptr; u.ldp = preact.ld;
