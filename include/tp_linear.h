@@ -376,11 +376,13 @@ typedef struct { void* ptr; int64_t ld, stride; } tp_factor_out_t;
  *   c, y     : [m, n], fp32 or bf16 each: the shared product (tp_linear_fwd with TP_EPI_NONE) and the output.  y may be c itself (same address, type and
  *              leading dimension), else the two must not overlap (TP_ERR_SHAPE).   bias, epi, preact: as in tp_linear_fwd.
  *   v        : optional fp32 [m, rank], rows rank apart: V, saved for backward (rows without an adapter are not written).
- *   workspace: >= tp_adapter_workspace_size(.., TP_PASS_FWD, ..) bytes, 16-byte aligned.
+ *   workspace: >= tp_adapter_workspace_size(.., TP_PASS_FWD, ..) bytes, 16-byte aligned; one call's at a time.
+ * Apart from y over c no output may overlap an input or another output.
  * V is the rank's own sum.  Where the shared product is an additive partial (1D_ROW, 3D_GATHERED), so is this: every rank adds the part of its own
  * columns of A, the reduction that completes c completes it, and epi, preact and a bf16 y are refused as in tp_linear_fwd.
  * Defined by: the adapted layer X (W + s A^T B) under the partition of tp_linear_fwd (Section 2.2): A is cut like W's rows, B like W's columns.
- * V is fp32; in the second product it stands as a sum of bf16 terms that is off by 2^-17 (bf16 y) or 2^-25 (fp32 y) of it.
+ * V is fp32; in the second product it stands as a sum of bf16 terms that is off by 2^-17 (bf16 y) or 2^-25 (fp32 y) of it.  What an infinite element of B
+ * reaches may therefore be NaN where the formula says infinity (in backward: what one of A, X or dY reaches in dX, dA or dB).
  * Errors: TP_ERR_NULL, TP_ERR_MODE, TP_ERR_GRID, TP_ERR_SHAPE (also: rank, pool or segment counts out of range, or more than 2^22 tiles of 16 rows of
  * short segments or 64 of long ones), TP_ERR_ALIGN, TP_ERR_DTYPE,
  * TP_ERR_WORKSPACE, TP_ERR_HIP; nothing is launched unless every check has passed.

@@ -333,6 +333,24 @@ bool look(PyObject* o, PyObject* want, Devices* at) {
     return false;
 }
 
+bool numel(PyObject* o, int64_t* n) { return call0(o, s_numel, n); }
+// a tensor (others are taken as they are) has at least `want` elements, one behind the other
+bool flat(PyObject* t, int64_t want, const char* what) {
+    bool tensor;
+    if (t == Py_None || PyLong_Check(t)) return true;
+    if (!is_tensor(t, &tensor)) return false;
+    if (!tensor) return true;
+    int64_t have;
+    if (!numel(t, &have)) return false;
+    Ref c(PyObject_CallMethodNoArgs(t, s_is_contiguous));
+    if (!c) return false;
+    if (have >= want && c.p == Py_True) return true;
+    PyErr_Format(PyExc_ValueError, "%s must be a contiguous tensor of at least %lld elements", what, (long long)want);
+    return false;
+}
+// a bias or its gradient
+bool to_flat(PyObject* o, PyObject* type, Devices* at, int64_t want, const char* what, void** p) { return look(o, type, at) && flat(o, want, what) && to_ptr(o, p); }
+
 // A block: None, a sequence as to_oblk() and to_cblk() take it, or a tensor on the current device of type `want` (null: fp32 or bf16, else 99)
 bool to_block(PyObject* o, PyObject* want, Devices* at, tp_oblk_t* b) {
     bool tensor = false;
@@ -402,7 +420,15 @@ bool to_dropout(PyObject* o, tp_dropout_t* d, Devices* at) {
     if (d->p == -1.0 && PyErr_Occurred()) return false;
     int64_t seed, offset;
     void* dev;
-    if (!to_i64(it[1], &seed) || !to_i64(it[2], &offset) || !look(it[3], nullptr, at) || !to_ptr(it[3], &dev) || !to_i64(it[4], &d->row0) || !to_i64(it[5], &d->col0)) return false;
+    if (!to_i64(it[1], &seed) || !to_i64(it[2], &offset) || !look(it[3], nullptr, at) || !flat(it[3], 1, "offset_dev") || !to_ptr(it[3], &dev) ||
+        !to_i64(it[4], &d->row0) || !to_i64(it[5], &d->col0))
+        return false;
+    if (it[3] != Py_None && !PyLong_Check(it[3])) {
+        bool tensor;
+        int64_t size = 8;
+        if (!is_tensor(it[3], &tensor) || (tensor && !call0(it[3], s_element_size, &size))) return false;
+        if (size != 8) { PyErr_SetString(PyExc_TypeError, "offset_dev must be a 64-bit integer"); return false; }
+    }
     d->seed = (uint64_t)seed;
     d->offset = (uint64_t)offset;
     d->offset_dev = static_cast<const uint64_t*>(dev);
@@ -411,24 +437,23 @@ bool to_dropout(PyObject* o, tp_dropout_t* d, Devices* at) {
 // dropout_fwd(dropout, x, bias, epi, residual, y, preact, rows, cols, stream)
 PyObject* dropout_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     tp_dropout_t d; tp_oblk_t x, y, pre; tp_cblk_t res; void *bias, *stream; int epi; int64_t rows, cols; Devices at;
-    if (!count(n, 10) || !to_dropout(a[0], &d, &at) || !to_block(a[1], nullptr, &at, &x) || !look(a[2], g_bf16, &at) || !to_ptr(a[2], &bias) ||
-        !to_int(a[3], &epi) || !to_input(a[4], &at, &res) || !to_block(a[5], nullptr, &at, &y) || !to_block(a[6], nullptr, &at, &pre) || !to_i64(a[7], &rows) || !to_i64(a[8], &cols) || !to_ptr(a[9], &stream))
+    if (!count(n, 10) || !to_dropout(a[0], &d, &at) || !to_block(a[1], nullptr, &at, &x) || !to_i64(a[7], &rows) || !to_i64(a[8], &cols) ||
+        !to_flat(a[2], g_bf16, &at, cols, "bias", &bias) || !to_int(a[3], &epi) || !to_input(a[4], &at, &res) || !to_block(a[5], nullptr, &at, &y) ||
+        !to_block(a[6], nullptr, &at, &pre) || !to_ptr(a[9], &stream))
         return nullptr;
     return answer([&] { return f_dropout_fwd(&d, x.ptr, x.ld, x.dtype, bias, epi, res, y, pre, rows, cols, stream); });
 }
 // dropout_bwd(dropout, dy, preact, dx, db, rows, cols, workspace, stream)
 PyObject* dropout_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     tp_dropout_t d; tp_cblk_t dy, pre, dx; void *db, *stream; int64_t rows, cols; Workspace ws; Devices at;
-    if (!count(n, 9) || !look(a[4], g_f32, &at) || !look(a[7], nullptr, &at) || !to_dropout(a[0], &d, &at) || !to_input(a[1], &at, &dy) ||
-        !to_input(a[2], &at, &pre) || !to_input(a[3], &at, &dx) || !to_ptr(a[4], &db) ||
-        !to_i64(a[5], &rows) || !to_i64(a[6], &cols) || !to_ws(a[7], &ws) || !to_ptr(a[8], &stream))
+    if (!count(n, 9) || !to_i64(a[5], &rows) || !to_i64(a[6], &cols) || !to_flat(a[4], g_f32, &at, cols, "db", &db) || !look(a[7], nullptr, &at) ||
+        !to_dropout(a[0], &d, &at) || !to_input(a[1], &at, &dy) || !to_input(a[2], &at, &pre) || !to_input(a[3], &at, &dx) || !to_ws(a[7], &ws) || !to_ptr(a[8], &stream))
         return nullptr;
     return answer([&] {
         return f_dropout_bwd(&d, dy.ptr, dy.ld, pre.ptr, pre.ld, const_cast<void*>(dx.ptr), dx.ld, db, rows, cols, ws.ptr, ws.bytes, stream);
     });
 }
 // A call's adapters: a sequence (offsets, ids, n_adapters, rank, scale, n_segments); n_segments None: as many as ids has
-bool numel(PyObject* o, int64_t* n) { return call0(o, s_numel, n); }
 bool to_adapters(PyObject* o, tp_adapters_t* a, Devices* at) {
     Ref s(PySequence_Fast(o, "adapters must be an Adapters"));
     if (!s) return false;
@@ -443,16 +468,6 @@ bool to_adapters(PyObject* o, tp_adapters_t* a, Devices* at) {
     if (!look(it[0], g_i32, at) || !look(it[1], g_i32, at) || !look(it[4], g_f32, at) || !to_ptr(it[0], &offsets) || !to_ptr(it[1], &ids) ||
         !to_int(it[2], &pool) || !to_int(it[3], &rank) || !to_ptr(it[4], &scale) || (it[5] != Py_None && !to_i64(it[5], &n)))
         return false;
-    auto flat = [&](PyObject* t, int64_t want, const char* what) {        // a tensor of at least that many elements, one behind the other
-        if (t == Py_None || PyLong_Check(t)) return true;
-        int64_t have;
-        if (!numel(t, &have)) return false;
-        Ref c(PyObject_CallMethodNoArgs(t, s_is_contiguous));
-        if (!c) return false;
-        if (have >= want && c.p == Py_True) return true;
-        PyErr_Format(PyExc_ValueError, "%s must be a contiguous tensor of %lld elements", what, (long long)want);
-        return false;
-    };
     if (it[5] == Py_None && it[1] != Py_None && !PyLong_Check(it[1]) && !numel(it[1], &n)) return false;
     if (n < 0 || n > INT32_MAX - 1) n = -1;                              // (the library answers)
     if (!flat(it[0], n > 0 ? n + 1 : 0, "offsets") || !flat(it[1], n > 0 ? n : 0, "ids") || !flat(it[4], pool, "scale")) return false;
@@ -507,12 +522,7 @@ struct Factors {
 // V: fp32 [rows, rank], one row behind the other
 bool to_v(PyObject* o, float** v, Devices* at) {
     void* p;
-    if (!look(o, g_f32, at) || !to_ptr(o, &p)) return false;
-    if (o != Py_None && !PyLong_Check(o)) {
-        Ref c(PyObject_CallMethodNoArgs(o, s_is_contiguous));
-        if (!c) return false;
-        if (c.p != Py_True) { PyErr_SetString(PyExc_ValueError, "v must be contiguous"); return false; }
-    }
+    if (!to_flat(o, g_f32, at, 0, "v", &p)) return false;
     *v = static_cast<float*>(p);
     return true;
 }
@@ -532,7 +542,7 @@ PyObject* adapter_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void *bias, *stream; float* v; Workspace ws; Devices at;
     if (!count(n, 16) || !to_struct(a[0], &grid) || !to_dims(a[1], &dims) || !to_int(a[2], &steps) || !to_adapters(a[3], &ad, &at) ||
         !x.fill(a[4], &at) || !f.fill(a[5], ad, &at) || !to_factor(a[6], &b, ad, g_bf16, &at) || !drop.fill(a[7], &at) ||
-        !to_block(a[8], nullptr, &at, &c) || !look(a[9], g_bf16, &at) || !to_ptr(a[9], &bias) || !to_int(a[10], &epi) ||
+        !to_block(a[8], nullptr, &at, &c) || !to_flat(a[9], g_bf16, &at, 0, "bias", &bias) || !to_int(a[10], &epi) ||
         !to_block(a[11], nullptr, &at, &y) || !to_block(a[12], nullptr, &at, &pre) || !to_v(a[13], &v, &at) ||
         !look(a[14], nullptr, &at) || !to_ws(a[14], &ws) || !to_ptr(a[15], &stream))
         return nullptr;

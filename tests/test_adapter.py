@@ -640,3 +640,77 @@ def test_calls_on_two_streams_at_once():
     torch.cuda.synchronize()
     for y in ys:
         assert torch.equal(y[0], y[1])
+
+
+@pytest.mark.gpu
+def test_arrays_that_are_too_short_or_of_another_type_are_refused():
+    """Before anything is launched: the outputs keep what they held."""
+    m, h, n, rank = 16, 64, 72, 16
+    grid, dims = T.Grid(T.MODE_1D_COL), (m, h, n)
+    cuda = lambda *s, dtype=BF: torch.zeros(*s, dtype=dtype, device="cuda")
+    i32 = lambda k: cuda(k, dtype=torch.int32)
+    ok = T.Adapters(i32(4), i32(3), 2, rank, cuda(2, dtype=F32))
+    y, dx = torch.full((m, n), 7.0, device="cuda"), torch.full((m, h), 7.0, device="cuda")
+    ws = cuda(1 << 22, dtype=torch.uint8)
+    fwd = lambda **k: T.tp_adapter_fwd(grid, dims, 1, k.get("ad", ok), [k.get("x", cuda(m, h))], [k.get("a", cuda(2, rank, h))], k.get("b", cuda(2, rank, n)), k.get("c", cuda(m, n)),
+                                       k.get("bias"), T.EPI_BIAS if "bias" in k else 0, y, v=k.get("v"), workspace=ws)
+    bwd = lambda **k: T.tp_adapter_bwd(grid, dims, 1, ok, [k.get("dy", cuda(m, n))], [cuda(2, rank, n)], a=cuda(2, rank, h), dx_base=cuda(m, h), dx=dx, x_own=k.get("x", cuda(m, h)),
+                                       da=k.get("da"), dy_own=cuda(m, n), v=k.get("v"), db=k.get("db"), workspace=ws)
+    ad = lambda **k: ok._replace(**k)
+    for call in (lambda: fwd(ad=ad(offsets=cuda(4, dtype=torch.int64))), lambda: fwd(ad=ad(ids=cuda(3, dtype=torch.int64))), lambda: fwd(ad=ad(scale=cuda(2))), lambda: fwd(x=cuda(m, h, dtype=F32)),
+                 lambda: fwd(a=cuda(2, rank, h, dtype=F32)), lambda: fwd(b=cuda(2, rank, n, dtype=torch.float16)), lambda: fwd(v=cuda(m, rank)), lambda: fwd(bias=cuda(n, dtype=F32)),
+                 lambda: bwd(da=cuda(2, rank, h)), lambda: bwd(db=cuda(2, rank, n), v=cuda(m, rank, dtype=F32)), lambda: bwd(dy=cuda(m, n, dtype=F32))):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: fwd(ad=ad(offsets=i32(3))), lambda: fwd(ad=ad(n_segments=4)), lambda: fwd(ad=ad(offsets=i32(8)[::2])), lambda: fwd(ad=ad(scale=cuda(1, dtype=F32))),
+                 lambda: fwd(a=cuda(3, rank, h)), lambda: fwd(a=cuda(2, 8, h)), lambda: fwd(a=cuda(rank, h)), lambda: fwd(a=cuda(2, h, rank).transpose(1, 2)),
+                 lambda: fwd(x=cuda(h, m).t()), lambda: fwd(v=cuda(m, 2 * rank, dtype=F32)[:, :rank]), lambda: fwd(bias=cuda(2 * n)[::2])):
+        with pytest.raises(ValueError):
+            call()
+    assert _st(lambda: fwd(a=cuda(1, rank, h).expand(2, rank, h))) == 4 and _st(lambda: fwd(c=cuda(m, n, dtype=torch.float16))) == 6
+    torch.cuda.synchronize()
+    assert (y == 7).all() and (dx == 7).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,rank,p", [(3, 128, 0.0), (5, 96, 0.25), (260, 40, 0.0)])
+def test_first_call_inside_a_capture(m, rank, p):
+    """A graph may be captured with no call before it: each replay gives what an eager call gives afterwards."""
+    g = _g(31)
+    h, n = 136, 200
+    grid, dims = T.Grid(T.MODE_1D_COL), (m, h, n)
+    x, a, b, c = _strided(g, m, h), _strided(g, 1, rank, h), _strided(g, 1, rank, n), _strided(g, m, n, dtype=F32)
+    ad = T.Adapters(torch.tensor([0, m], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), 1, rank)
+    ws = torch.empty(T.tp_adapter_workspace_size(grid, dims, T.PASS_FWD, ad), dtype=torch.uint8, device="cuda")
+    y, z = (torch.full((m, n), 7.0, device="cuda") for _ in range(2))
+    call = lambda out: T.tp_adapter_fwd(grid, dims, 1, ad, [x], [a], b, c, None, 0, out, dropout=T.Dropout(p, 5) if p else None, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(y)
+    for _ in range(3):
+        x.normal_(generator=g)
+        y.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        call(z)
+        torch.cuda.synchronize()
+        assert torch.equal(y, z)
+
+
+@pytest.mark.gpu
+def test_an_infinite_factor_stays_in_its_columns():
+    """One infinite element of B: its column alone is not finite, in the rows of its adapter alone."""
+    m, h, n, rank = 70, 64, 136, 16
+    g = _g(33)
+    grid, dims = T.Grid(T.MODE_1D_COL), (m, h, n)
+    x, a, b, c = _strided(g, m, h), _strided(g, 2, rank, h), _strided(g, 2, rank, n), _strided(g, m, n)
+    ad = T.Adapters(torch.tensor([0, 30, m], dtype=torch.int32, device="cuda"), torch.tensor([0, 1], dtype=torch.int32, device="cuda"), 2, rank)
+    ws = torch.empty(T.tp_adapter_workspace_size(grid, dims, T.PASS_FWD, ad), dtype=torch.uint8, device="cuda")
+    y, z = (torch.full((m, n), 7.0, dtype=BF, device="cuda") for _ in range(2))
+    T.tp_adapter_fwd(grid, dims, 1, ad, [x], [a], b, c, None, 0, y, workspace=ws)
+    b[1, 5, 77] = float("inf")
+    T.tp_adapter_fwd(grid, dims, 1, ad, [x], [a], b, c, None, 0, z, workspace=ws)
+    hit = torch.zeros(m, n, dtype=torch.bool, device="cuda")
+    hit[30:, 77] = True
+    assert torch.equal(y[~hit], z[~hit]) and not torch.isfinite(z[hit]).any()

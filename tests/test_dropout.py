@@ -300,3 +300,25 @@ def test_captured_graph_draws_a_new_mask_each_replay():
     T.tp_dropout_fwd(T.Dropout(0.3, 77, 3, step), x, None, T.EPI_NONE, y)
     T.tp_dropout_fwd(T.Dropout(0.3, 77, 2), x, None, T.EPI_NONE, dx)
     assert torch.equal(y, dx)
+
+
+@pytest.mark.gpu
+def test_arrays_that_are_too_short_or_of_another_type_are_refused():
+    """Before anything is launched: y keeps what it held."""
+    x, y = torch.zeros(4, 64, device="cuda"), torch.full((4, 64), 7.0, device="cuda")
+    bf = lambda n: torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    fwd = lambda d=T.Dropout(0.1, 1), **k: T.tp_dropout_fwd(d, k.get("x", x), k.get("bias"), T.EPI_BIAS if "bias" in k else T.EPI_NONE, y, residual=k.get("res"))
+    at = lambda t: T.Dropout(0.1, 1, 0, t)
+    for error, call in ((ValueError, lambda: fwd(bias=bf(56))), (ValueError, lambda: fwd(bias=bf(128)[::2])), (ValueError, lambda: fwd(bias=bf(1).expand(64))),
+                        (TypeError, lambda: fwd(bias=torch.zeros(64, device="cuda"))), (TypeError, lambda: fwd(res=x)), (ValueError, lambda: fwd(x=torch.zeros(64, 4, device="cuda").t())),
+                        (TypeError, lambda: fwd(at(torch.zeros(1, dtype=torch.int32, device="cuda")))), (ValueError, lambda: fwd(at(torch.zeros(0, dtype=torch.int64, device="cuda")))),
+                        (TypeError, lambda: T.tp_dropout_bwd(T.Dropout(0.1, 1), x, bf((4, 64)))),
+                        (ValueError, lambda: T.tp_dropout_bwd(T.Dropout(0.1, 1), bf((4, 64)), bf((4, 64)), db=torch.zeros(56, device="cuda"))),
+                        (TypeError, lambda: T.tp_dropout_bwd(T.Dropout(0.1, 1), bf((4, 64)), bf((4, 64)), db=bf(64)))):
+        with pytest.raises(error):
+            call()
+    with pytest.raises(T.TpError) as e:
+        fwd(x=x.half())
+    assert e.value.status == 6
+    torch.cuda.synchronize()
+    assert (y == 7).all()
