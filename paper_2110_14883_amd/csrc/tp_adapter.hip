@@ -265,6 +265,43 @@ __global__ __launch_bounds__(64 * down_waves(MT, RB, DROP)) void tp_adapter_down
 }
 
 // ---------------------------------------------------------------------------------------------
+// The shares' planes of dA and dB (grad, below) added in order, eight on their way at a time; a share without rows has none.  Four elements a thread, block `block` of
+// finish_share().  In a backward pass that also wants dX this is done by workgroups of *up* behind its tiles, otherwise by a launch of its own (backward of
+// 32896 x 640 over 2 x 2560, 8 ranks 101 us against 105; 16384 x 4096 x 4096, 16 ranks 178.3 against 178.9).
+// ---------------------------------------------------------------------------------------------
+__host__ __device__ inline int finish_blocks_each(const GradArgs& p, int threads) {
+    const int most = p.sides > 1 && p.side[1].cols > p.side[0].cols ? p.side[1].cols : p.side[0].cols;
+    return (most * p.rank / 4 + threads - 1) / threads;                  // (up to 2^21 columns)
+}
+__device__ __forceinline__ void finish_share(const GradArgs& p, unsigned block) {
+    const unsigned each = (unsigned)finish_blocks_each(p, blockDim.x), y = block / each;
+    if (y >= (unsigned)(p.seg.pool * p.sides)) return;
+    const int which = y >= (unsigned)p.seg.pool, a = which ? y - p.seg.pool : y;
+    const GradSide& q = p.side[which];
+    const unsigned at = ((block - y * each) * blockDim.x + threadIdx.x) * 4, plane = (unsigned)(p.rank * q.cols);      // (up to 128 x 2^21)
+    if (at >= plane) return;
+    const unsigned k = at / (unsigned)q.cols, cc = at - k * (unsigned)q.cols;
+    const float* const part = q.part + (int64_t)a * p.shares * plane + at;
+    const unsigned total = (unsigned)p.units[a], shares = (unsigned)p.shares;
+    f32x4_t* const to = reinterpret_cast<f32x4_t*>(q.out + a * q.stride + k * q.ldo + cc);
+    f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int z0 = 0; z0 < p.shares; z0 += 8) {
+        f32x4_t v[8];
+#pragma unroll
+        for (int z = 0; z < 8; ++z) {
+            const int y = z0 + z;
+            v[z] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            if (y < p.shares && (total >= shares || total * y / shares < total * (y + 1) / shares))
+                v[z] = *reinterpret_cast<const f32x4_t*>(part + (int64_t)y * plane);
+        }
+#pragma unroll
+        for (int z = 0; z < 8; ++z) s += v[z];
+    }
+    if (p.accumulate) s = *to + s;
+    *to = s;
+}
+
+// ---------------------------------------------------------------------------------------------
 // up.  A workgroup has a tile of rows and, a wave each, strips of 128 columns.  It first lays V's terms out in LDS, as the rows of the second product's
 // left operand: first terms, second terms (third ones) of a row's ranks one behind the other, so that for up to 16 ranks two terms fill one matrix
 // instruction's 32 k.  A wave turns its strip of the factor into matrix operands once, eight 16-column blocks, so that a lane ends up with eight
@@ -448,11 +485,15 @@ __device__ __forceinline__ void lay_terms(char* low, int r, int q, const float (
 }
 
 template <int GP, int TERMS, bool DROP, bool C32>
-__global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p) {
+__global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p, const GradArgs fin) {
     using Strip = UpStrip<GP, TERMS, DROP, C32>;
     constexpr int AHEAD = UpShape<GP, TERMS>::template AHEAD<C32>;
     extern __shared__ __attribute__((aligned(16))) char low[];
     const int strip = uni(blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6));
+    if (blockIdx.x >= (unsigned)p.tiles) {
+        finish_share(fin, (blockIdx.x - p.tiles) * gridDim.y + blockIdx.y);
+        return;
+    }
     preload(p);
     Tile t;
     if (!find_tile(p.seg, blockIdx.x, p.tile, t)) return;
@@ -733,31 +774,7 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
         }
     }
 }
-// the shares' planes added in order, eight on their way at a time; a share without rows has none
-__global__ __launch_bounds__(64) void tp_adapter_grad_finish_kernel(const GradArgs p) {
-    const int which = blockIdx.y >= (unsigned)p.seg.pool, a = which ? blockIdx.y - p.seg.pool : blockIdx.y;
-    const GradSide& q = p.side[which];
-    const int64_t at = ((int64_t)blockIdx.x * 64 + threadIdx.x) * 4;
-    if (at >= (int64_t)p.rank * q.cols) return;
-    const int k = (int)(at / q.cols), cc = (int)(at - (int64_t)k * q.cols);
-    const int64_t total = p.units[a];
-    f32x4_t* const to = reinterpret_cast<f32x4_t*>(q.out + a * q.stride + k * q.ldo + cc);
-    f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int z0 = 0; z0 < p.shares; z0 += 8) {
-        f32x4_t v[8];
-#pragma unroll
-        for (int z = 0; z < 8; ++z) {
-            const int y = z0 + z;
-            v[z] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-            if (y < p.shares && total * y / p.shares < total * (y + 1) / p.shares)
-                v[z] = *reinterpret_cast<const f32x4_t*>(q.part + ((int64_t)a * p.shares + y) * p.rank * q.cols + at);
-        }
-#pragma unroll
-        for (int z = 0; z < 8; ++z) s += v[z];
-    }
-    if (p.accumulate) s = *to + s;
-    *to = s;
-}
+__global__ __launch_bounds__(64) void tp_adapter_grad_finish_kernel(const GradArgs p) { finish_share(p, blockIdx.x); }
 
 // Kernels with more LDS than a launch has by default: said once on every device (the same value every time)
 template <class K>
@@ -788,15 +805,18 @@ hipError_t down_rank(const DownArgs& a, hipStream_t s) {
 }
 
 template <int GP, int TERMS>
-hipError_t up_as(const UpArgs& a, hipStream_t s) {
-    const int strips = (a.cols + 127) / 128, waves = up_waves(strips, a.tiles);
-    const dim3 grid((unsigned)a.tiles, (unsigned)((strips + waves - 1) / waves)), block(64 * waves);
+hipError_t up_as(const UpArgs& a, const GradArgs* fin, hipStream_t s) {
+    const int strips = (a.cols + 127) / 128, waves = up_waves(strips, a.tiles), y = (strips + waves - 1) / waves;
+    // (planes to add are there only where *grad* has under 512 workgroups: a few thousand more)
+    const int64_t more = fin ? ((int64_t)finish_blocks_each(*fin, 64 * waves) * fin->seg.pool * fin->sides + y - 1) / y : 0;
+    const dim3 grid((unsigned)(a.tiles + more), (unsigned)y), block(64 * waves);
     const size_t lds = (size_t)a.tile * UpShape<GP, TERMS>::ROW;
     return launch_kernel(a.c_f32 ? (a.dropped ? tp_adapter_up_kernel<GP, TERMS, true, true> : tp_adapter_up_kernel<GP, TERMS, false, true>)
-                                 : (a.dropped ? tp_adapter_up_kernel<GP, TERMS, true, false> : tp_adapter_up_kernel<GP, TERMS, false, false>), grid, block, lds, s, a);
+                                 : (a.dropped ? tp_adapter_up_kernel<GP, TERMS, true, false> : tp_adapter_up_kernel<GP, TERMS, false, false>), grid, block, lds, s, a,
+                         fin ? *fin : GradArgs{});
 }
 template <int GP>
-hipError_t up(const UpArgs& a, hipStream_t s) { return a.out_f32 ? up_as<GP, 3>(a, s) : up_as<GP, 2>(a, s); }
+hipError_t up(const UpArgs& a, const GradArgs* fin, hipStream_t s) { return a.out_f32 ? up_as<GP, 3>(a, fin, s) : up_as<GP, 2>(a, fin, s); }
 
 }  // namespace
 
@@ -831,22 +851,18 @@ hipError_t launch_few(const DownArgs& d, const UpArgs& u, hipStream_t s) {
          : u.rank <= 64 ? pick(std::integral_constant<int, 4>{}) : pick(std::integral_constant<int, 8>{});
 }
 
-hipError_t launch_up(const UpArgs& a, hipStream_t s) {
-    if (a.tiles < 1) return hipSuccess;
-    return a.rank <= 16 ? up<2>(a, s) : a.rank <= 32 ? up<4>(a, s) : a.rank <= 64 ? up<8>(a, s) : up<16>(a, s);
+hipError_t launch_up(const UpArgs& a, const GradArgs* fin, hipStream_t s) {
+    return a.rank <= 16 ? up<2>(a, fin, s) : a.rank <= 32 ? up<4>(a, fin, s) : a.rank <= 64 ? up<8>(a, fin, s) : up<16>(a, fin, s);
 }
 
-hipError_t launch_grad(const GradArgs& a, hipStream_t s) {
+hipError_t launch_grad(const GradArgs& a, bool finish, hipStream_t s) {
     const int strips0 = (a.side[0].cols + 127) / 128, strips = strips0 + (a.sides > 1 ? (a.side[1].cols + 127) / 128 : 0);
     const int rb = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4, chunks = (a.rank + 16 * rb - 1) / (16 * rb);
     const int64_t blocks = (int64_t)strips * chunks * a.shares * a.seg.pool;      // (the caller has looked at how many)
     if (hipError_t e = launch_kernel(rb == 1 ? tp_adapter_grad_kernel<1> : rb == 2 ? tp_adapter_grad_kernel<2> : tp_adapter_grad_kernel<4>,
-                                     dim3((unsigned)blocks), dim3(64 * GRAD_WAVES), 0, s, a, strips0, strips); e != hipSuccess || a.shares == 1)
+                                     dim3((unsigned)blocks), dim3(64 * GRAD_WAVES), 0, s, a, strips0, strips); e != hipSuccess || a.shares == 1 || !finish)
         return e;
-    int64_t most = 0;
-    for (int i = 0; i < a.sides; ++i) most = a.side[i].cols > most ? a.side[i].cols : most;
-    const int64_t x = (most * a.rank / 4 + 63) / 64;
-    return launch_kernel(tp_adapter_grad_finish_kernel, dim3((unsigned)x, (unsigned)(a.seg.pool * a.sides)), dim3(64), 0, s, a);
+    return launch_kernel(tp_adapter_grad_finish_kernel, dim3((unsigned)((int64_t)finish_blocks_each(a, 64) * a.seg.pool * a.sides)), dim3(64), 0, s, a);
 }
 
 }  // namespace tpl

@@ -114,7 +114,8 @@ struct UpArgs {
     int32_t dropped;
     DropArgs drop;
 };
-hipError_t launch_up(const UpArgs& args, hipStream_t stream);
+struct GradArgs;
+hipError_t launch_up(const UpArgs& args, const GradArgs* add, hipStream_t stream);      // add: shares of launch_grad() to add up besides, or null
 // Both in one launch, without dropout, tiles of 16 rows (V is not kept but for v_out)
 hipError_t launch_few(const DownArgs& down, const UpArgs& up, hipStream_t stream);
 // Waves of a workgroup of launch_up, a strip of 128 columns each: as few idle ones as possible, about four; with few tiles a strip a workgroup
@@ -141,7 +142,7 @@ struct GradArgs {
     DropArgs drop;
     int32_t* units;                      // [pool] of shares > 1
 };
-hipError_t launch_grad(const GradArgs& args, hipStream_t stream);
+hipError_t launch_grad(const GradArgs& args, bool finish, hipStream_t stream);         // without `finish` several shares are left to launch_up()
 
 // tile ids: macro-tile shapes the GEMM kernel is instantiated for
 enum TileId { TILE_256x256 = 1, TILE_128x256 = 2, TILE_256x128 = 3, TILE_128x128 = 4,

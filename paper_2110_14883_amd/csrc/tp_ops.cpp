@@ -220,7 +220,7 @@ int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
     if (adapters->n_segments == 0) return TP_OK;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (few) return launch_few(d, u, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
-    return launch_down(d, stream) != hipSuccess || launch_up(u, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
+    return launch_down(d, stream) != hipSuccess || launch_up(u, nullptr, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
 }
 
 int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, const tp_adapters_t* adapters, const tp_cblk_t* dy_blocks,
@@ -277,10 +277,10 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
     if (!ws_ok(need.all(), workspace, workspace_bytes)) return TP_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     // (dA and dB before dX: dY, which U has just read, may still be in the last cache)
-    const bool some = adapters->n_segments > 0;
+    const bool some = adapters->n_segments > 0, up = some && dx.ptr, add_in_up = up && g.sides && g.shares > 1;
     if (some && want_u && launch_down(d, stream) != hipSuccess) return TP_ERR_HIP;
-    if (g.sides && launch_grad(g, stream) != hipSuccess) return TP_ERR_HIP;
-    return some && dx.ptr && launch_up(u, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
+    if (g.sides && launch_grad(g, !add_in_up, stream) != hipSuccess) return TP_ERR_HIP;
+    return up && launch_up(u, add_in_up ? &g : nullptr, stream) != hipSuccess ? TP_ERR_HIP : TP_OK;
 }
 
 int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_dtype, const void* bias, int epi, tp_cblk_t residual, tp_oblk_t y,
