@@ -122,8 +122,12 @@ __device__ __forceinline__ f32x4_t mfma(const u32x4_t& a, const u32x4_t& b, cons
 // direct-to-LDS loads of 8 whole lines each, with no barrier in the loop.  (Fragments loaded straight into registers, 64 bytes of 16 rows an
 // instruction, kept the address path busy longer: 16384 x 4096, 16 ranks 34.2 us against 28.5, 32896 x 2 x 2560 in 24 segments 67 / 46.)
 // ---------------------------------------------------------------------------------------------
-// (with a mask to draw, the waves count for more than the slots)
-constexpr int down_waves(int mt, int rb, bool drop) { return mt + rb <= (drop ? 8 : 5) ? 8 : 4; }
+// (with a mask to draw, the waves count for more than the slots.  At 128 ranks a slot is 24 KB: six waves with one each 16384 x 4096 46.1 us, four 52.4, three with
+// two 45.6, and 7731 x 7296 with a mask, forward, 91.8 / 95.3 / 105; tiles of 32 rows, 731 of 2496: four with two slots 9.2, eight with one 10.4, with a mask 553 of 3968 17.6 / 14.2.)
+constexpr int down_waves(int mt, int rb, bool drop) {
+    if (rb == 8) return mt == 4 ? 6 : mt == 2 && drop ? 8 : 4;
+    return mt + rb <= (drop ? 8 : 5) ? 8 : 4;
+}
 template <int MT, int RB, bool DROP> struct DownShape {
     static constexpr int WAVES = down_waves(MT, RB, DROP);
     static constexpr int SLOT = (MT + RB) * 2048;                                               // a unit: lines of 16 MT rows, of 16 RB ranks
@@ -515,10 +519,21 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p, cons
             float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             if (8 * q < p.rank) {
                 const int64_t at = (int64_t)(t.row0 + r) * p.rank + 8 * q;
-                for (int z = 0; z < p.splits; ++z) {
-                    const f32x4_t *src = reinterpret_cast<const f32x4_t*>(p.v + z * p.plane + at), a = src[0], b = src[1];
+                for (int z0 = 0; z0 < p.splits; z0 += 4) {               // (four planes on their way at a time)
+                    f32x4_t a[4], b[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) { v[k] += a[k]; v[4 + k] += b[k]; }
+                    for (int z = 0; z < 4; ++z) {
+                        a[z] = b[z] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                        if (z0 + z < p.splits) {
+                            const f32x4_t* src = reinterpret_cast<const f32x4_t*>(p.v + (z0 + z) * p.plane + at);
+                            a[z] = src[0];
+                            b[z] = src[1];
+                        }
+                    }
+#pragma unroll
+                    for (int z = 0; z < 4; ++z)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) { v[k] += a[z][k]; v[4 + k] += b[z][k]; }
                 }
                 if (p.v_out && blockIdx.y == 0) {
                     f32x4_t* const to = reinterpret_cast<f32x4_t*>(p.v_out + at);
@@ -689,7 +704,7 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
         for (int j = 0; j < 8; ++j) rows[j] = buf_load16(rr, in ? (uint32_t)(((8 * g + j) * q.ldr + n) * 2) : OOB_OFFSET);
         uint32_t first[RB][8];
         auto plane = [&](int z, int i, int j) __attribute__((always_inline)) {
-            const __amdgpu_buffer_rsrc_t rl = make_rsrc(q.l + z * q.plane + (int64_t)row * p.rank, (int64_t)have * p.rank * 4);
+            const __amdgpu_buffer_rsrc_t rl = make_rsrc(q.l + z * q.plane + (int64_t)row * p.rank, z < q.splits ? (int64_t)have * p.rank * 4 : 0);
             const int k = rank0 + 16 * i + c;
             return __builtin_amdgcn_raw_buffer_load_b32(rl, k < p.rank ? ((8 * g + j) * p.rank + k) * 4 : (int)OOB_OFFSET, 0, 0);
         };
@@ -710,11 +725,22 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
         for (int i = 0; i < RB; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = as_float(first[i][j]);
-        for (int z = 1; z < q.splits; ++z)
+        constexpr int MORE = RB == 1 ? 4 : 2;                    // planes on their way at a time
+        for (int z0 = 1; z0 < q.splits; z0 += MORE) {
+            uint32_t next[MORE][RB][8];
 #pragma unroll
-            for (int i = 0; i < RB; ++i)
+            for (int z = 0; z < MORE; ++z)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] += as_float(plane(z, i, j));
+                for (int i = 0; i < RB; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) next[z][i][j] = plane(z0 + z, i, j);
+#pragma unroll
+            for (int z = 0; z < MORE; ++z)
+#pragma unroll
+                for (int i = 0; i < RB; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[i][j] += as_float(next[z][i][j]);
+        }
         transpose8(rows, r);
 #pragma unroll
         for (int i = 0; i < RB; ++i) {

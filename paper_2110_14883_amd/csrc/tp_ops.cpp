@@ -70,16 +70,18 @@ int64_t most_tiles(int64_t rows, int64_t segments, int tile) {
     return (rows + some * (tile - 1)) / tile;
 }
 // How the products run.
-//   down: short segments (up to 24 rows on average) take tiles of 16 rows, others of 64, or of 32 where 64 make at most 128 tiles, leave the CU with the most
-//     tiles more rows (the start of one counted as eight), or there are more than 64 ranks.  us with 64 / 32: 16384 x 4096, 16 ranks 29.6 / 36.5; 32896 x 2 x
+//   down: short segments (up to 24 rows on average) take tiles of 16 rows, others of 64, or of 32 where 64 make at most 128 tiles or leave the CU with the most
+//     tiles more rows (the start of one counted as eight).  us with 64 / 32: 16384 x 4096, 16 ranks 29.6 / 36.5; 32896 x 2 x
 //     2560 in 24 segments 50.2 / 46.3; 2048 x 4 x 2048, 64 ranks 15.6 / 15.6, and up 21.5 / 19.3 for half the planes.  K is shared by as many workgroups
-//     as make one for every CU, while each has eight units of 64.
+//     as make one for every CU, while each has eight units of 64, and while the planes are fewer than what reads them pays for (up, and in backward grad, once
+//     for each of its strips; a multiple of four above four, as those are read): us with up to 4 / 8 / 12 planes, forward of 553 rows, 3968 to 432 columns, 64
+//     ranks 24.5 / 21.4 / 22.5, 128 ranks 39.5 / - / 35.8; backward of 731 rows of 1504 and 2496 columns, 64 ranks 32.3 / 35.6 / -, 128 ranks 44.9 / 47.9 / -.
 //   up: tiles of 32, 64 or 128 rows, whichever leaves the CU with the most workgroups (two at least, or there are too few loads under way) the
 //     fewest rows, the start of a workgroup counted as ten.  us with 32 / 64 / 128: 16384 x 4096 fp32 with dropout, 16 ranks
 //     118 / 110 / 101; 6000 x 4096 in 12 segments with GeLU, 32 ranks 44.9 / 47.6 / 45.4; 2048 x 8192, 64 ranks 25.1 / 21.8 / 25.2; 32896 x 640 in 24 segments
 //     19.2 / 21.6 / 24.3.
 struct Split { int tile, splits; int64_t tiles; int up_tile; int64_t up_tiles; };
-Split plan_products(int64_t rows, int64_t segments, int64_t k, int n_steps, int64_t up_cols, int rank) {
+Split plan_products(int64_t rows, int64_t segments, int64_t k, int n_steps, int64_t up_cols, int rank, bool bwd) {
     Split s;
     const bool brief = rows <= 24 * std::max<int64_t>(1, std::min(rows, segments));
     auto tiles = [&](int tile) { return std::max<int64_t>(1, most_tiles(rows, segments, tile)); };
@@ -100,7 +102,8 @@ Split plan_products(int64_t rows, int64_t segments, int64_t k, int n_steps, int6
     s.tiles = tiles(s.tile);
     s.up_tiles = tiles(s.up_tile);
     const int64_t units = (k + 63) / 64 * n_steps;
-    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / s.tiles, units / 8, 16}));
+    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / s.tiles, units / 8, 16, bwd ? std::max(4, 256 / rank) : std::max(8, 512 / rank)}));
+    if (s.splits > 4) s.splits &= ~3;
     return s;
 }
 // A launch's threads are counted in 32 bits: at most 2^22 tiles, and 2^23 workgroups of the gradients
@@ -116,22 +119,26 @@ bool in_one_launch(const Split& s, int64_t rows, int64_t segments, int64_t facto
     const int64_t most = s.tiles >= 192 ? 1 << 21 : s.tiles >= 80 ? 1 << 19 : 1 << 17;
     return factor <= (rows > 8 * segments ? most / 4 : most);
 }
-// Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) for two a CU (four: 63 us for 55, and more planes), 128 rows a share at least
+// Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) of the adapters that can have rows for two a CU (four: 63 us
+// for 55, and more planes), but of four units of 32 rows (one a wave) at least, and planes for at most 64 adapters where that is more than
+// the whole pool would ask for.  Backward in us, by rows and the whole pool before: 222 rows in 29 segments, 56 ranks 34.5 -> 24; 8814 rows, two of 12 adapters
+// with some, 32 ranks 83.4 -> 67.9.
 int64_t grad_blocks(int64_t cols, int pool, int rank) { return (cols + 127) / 128 * ((rank + 63) / 64) * pool; }
-int plan_grad(int64_t rows, int64_t cols, int pool, int rank) {
-    const int64_t blocks = grad_blocks(cols, pool, rank);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(512 + blocks - 1) / blocks, rows / 128, 32}));
+int plan_grad(int64_t rows, int64_t segments, int64_t cols, int pool, int rank) {
+    auto enough = [&](int64_t adapters) { const int64_t blocks = grad_blocks(cols, 1, rank) * adapters; return (512 + blocks - 1) / blocks; };
+    const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(pool, segments)), most = std::max<int64_t>(enough(pool), 64 / pool);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({enough(busy), most, most_tiles(rows, segments, 32) / 4, 32}));
 }
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 // the workspace, in this order
 struct Space { size_t low, da, db, units; size_t all() const { return padded(low) + padded(da) + padded(db) + padded(units); } };
 Space space_fwd(const Map& f, const tp_adapters_t* a) {
-    const Split s = plan_products(f.m, a->n_segments, f.k, f.n_steps, f.n, a->rank);
+    const Split s = plan_products(f.m, a->n_segments, f.k, f.n_steps, f.n, a->rank, false);
     return Space{(size_t)s.splits * (size_t)f.m * a->rank * 4, 0, 0, 0};
 }
 Space space_bwd(const Map& f, const Map& x, const tp_adapters_t* a) {
-    const Split s = plan_products(x.m, a->n_segments, x.k, x.n_steps, x.n, a->rank);
-    const size_t shares = (size_t)plan_grad(x.m, x.n + f.n, a->n_adapters, a->rank), each = shares * a->n_adapters * a->rank * 4;
+    const Split s = plan_products(x.m, a->n_segments, x.k, x.n_steps, x.n, a->rank, true);
+    const size_t shares = (size_t)plan_grad(x.m, a->n_segments, x.n + f.n, a->n_adapters, a->rank), each = shares * a->n_adapters * a->rank * 4;
     Space w{(size_t)s.splits * (size_t)x.m * a->rank * 4, 0, 0, 0};
     if (shares > 1) { w.da = each * x.n; w.db = each * f.n; w.units = (size_t)a->n_adapters * 4; }
     return w;
@@ -193,7 +200,7 @@ int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
         if (epi != TP_EPI_NONE || preact.ptr) return TP_ERR_MODE;
         if (y.ptr && y.dtype != TP_F32) return TP_ERR_DTYPE;
     }
-    const Split sp = plan_products(s.m, adapters->n_segments, s.k, s.n_steps, s.n, adapters->rank);
+    const Split sp = plan_products(s.m, adapters->n_segments, s.k, s.n_steps, s.n, adapters->rank, false);
     if (int e = check_tiles(sp)) return e;
     const Space need = space_fwd(s, adapters);
     float* const planes = v && sp.splits == 1 ? v : static_cast<float*>(workspace);
@@ -237,7 +244,7 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
     if ((dx.ptr && !a) || (da.ptr && !x_own) || (db.ptr && (!dy_own || !v))) return TP_ERR_NULL;
     if (!aligned16(v)) return TP_ERR_ALIGN;
     if (dx.ptr && x.partial && dx.dtype != TP_F32) return TP_ERR_DTYPE;
-    const Split sp = plan_products(x.m, adapters->n_segments, x.k, x.n_steps, x.n, adapters->rank);
+    const Split sp = plan_products(x.m, adapters->n_segments, x.k, x.n_steps, x.n, adapters->rank, true);
     if (int e = check_tiles(sp)) return e;
     if (grad_blocks(x.n + f.n, adapters->n_adapters, adapters->rank) > kMostGradBlocks) return TP_ERR_SHAPE;
     const Space need = space_bwd(f, x, adapters);
@@ -270,7 +277,7 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
         if (int e = side(planes, sp.splits, *x_own, x.n, drop != nullptr, da, padded(need.low))) return e;
     if (db.ptr)
         if (int e = side(v, 1, *dy_own, f.n, 0, db, padded(need.low) + padded(need.da))) return e;
-    g.rank = adapters->rank; g.shares = plan_grad(x.m, x.n + f.n, adapters->n_adapters, adapters->rank); g.accumulate = accumulate != 0;
+    g.rank = adapters->rank; g.shares = plan_grad(x.m, adapters->n_segments, x.n + f.n, adapters->n_adapters, adapters->rank); g.accumulate = accumulate != 0;
     g.scale = adapters->scale; g.seg = segments(adapters, x.m); g.drop = mask;
     g.units = reinterpret_cast<int32_t*>(at + padded(need.low) + padded(need.da) + padded(need.db));
     if (!want_u && !db.ptr) return TP_OK;
