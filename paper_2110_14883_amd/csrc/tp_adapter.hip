@@ -493,7 +493,8 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p, cons
     using Strip = UpStrip<GP, TERMS, DROP, C32>;
     constexpr int AHEAD = UpShape<GP, TERMS>::template AHEAD<C32>;
     extern __shared__ __attribute__((aligned(16))) char low[];
-    const int strip = uni(blockIdx.y * (blockDim.x >> 6) + (threadIdx.x >> 6));
+    const int w = uni(threadIdx.x >> 6), strip = w < p.waves ? blockIdx.y * p.waves + w : 1 << 20;
+    const bool mine = strip * 128 < p.cols;
     if (blockIdx.x >= (unsigned)p.tiles) {
         finish_share(fin, (blockIdx.x - p.tiles) * gridDim.y + blockIdx.y);
         return;
@@ -509,9 +510,11 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p, cons
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) st.load_c(cv[i], 16 * i);
     };
-    if (adapted) {
-        st.load_factor(f);
+    if (mine) {
+        if (adapted) st.load_factor(f);
         start_c();
+    }
+    if (adapted) {
         // V's terms; eight ranks of a row a thread
         const float scale = (p.scale ? p.scale[t.id] : 1.0f) * (DROP ? p.drop.factor : 1.0f);
         for (int i = threadIdx.x; i < t.rows * GP; i += blockDim.x) {
@@ -545,12 +548,10 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p, cons
             }
             lay_terms<GP, TERMS>(low, r, q, v);
         }
-        st.turn(f);
-    } else {
-        start_c();
+        if (mine) st.turn(f);
     }
     __syncthreads();
-    if (strip * 128 >= p.cols) return;
+    if (!mine) return;
     Mask m;
     if constexpr (DROP) m = open_mask(p.drop);
     const u32x4_t bias = st.load_bias();
@@ -832,13 +833,19 @@ hipError_t down_rank(const DownArgs& a, hipStream_t s) {
 
 template <int GP, int TERMS>
 hipError_t up_as(const UpArgs& a, const GradArgs* fin, hipStream_t s) {
-    const int strips = (a.cols + 127) / 128, waves = up_waves(strips, a.tiles), y = (strips + waves - 1) / waves;
+    const int strips = (a.cols + 127) / 128, strip_waves = up_waves(strips, a.tiles), y = (strips + strip_waves - 1) / strip_waves;
+    // (a workgroup of one strip has as many waves as V's terms keep busy, up to four: all of a call, forward of 553 rows of 3968 to 432 columns, 64 ranks 17.8 us, 21.4
+    // with one wave, 128 ranks 23.5 / 31.0; backward of 731 rows of 1504 and 2496 columns, 64 ranks 28.5 / 32.4,
+    // 128 ranks 40.6 / 45.0, and 44.9 with up to six)
+    const int waves = strip_waves > 1 ? strip_waves : a.tile * GP >= 256 ? 4 : (a.tile * GP + 63) / 64;
+    UpArgs args = a;
+    args.waves = strip_waves;
     // (planes to add are there only where *grad* has under 512 workgroups: a few thousand more)
     const int64_t more = fin ? ((int64_t)finish_blocks_each(*fin, 64 * waves) * fin->seg.pool * fin->sides + y - 1) / y : 0;
     const dim3 grid((unsigned)(a.tiles + more), (unsigned)y), block(64 * waves);
     const size_t lds = (size_t)a.tile * UpShape<GP, TERMS>::ROW;
     return launch_kernel(a.c_f32 ? (a.dropped ? tp_adapter_up_kernel<GP, TERMS, true, true> : tp_adapter_up_kernel<GP, TERMS, false, true>)
-                                 : (a.dropped ? tp_adapter_up_kernel<GP, TERMS, true, false> : tp_adapter_up_kernel<GP, TERMS, false, false>), grid, block, lds, s, a,
+                                 : (a.dropped ? tp_adapter_up_kernel<GP, TERMS, true, false> : tp_adapter_up_kernel<GP, TERMS, false, false>), grid, block, lds, s, args,
                          fin ? *fin : GradArgs{});
 }
 template <int GP>

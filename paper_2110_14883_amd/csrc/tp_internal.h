@@ -109,7 +109,7 @@ struct UpArgs {
     const void* bias; int32_t gelu;
     void* out; int64_t ldo; int32_t out_f32;
     void* pre; int64_t ldp;
-    int32_t tile, tiles;
+    int32_t tile, tiles, waves;          // (waves with a strip: set by launch_up)
     SegArgs seg;
     int32_t dropped;
     DropArgs drop;
