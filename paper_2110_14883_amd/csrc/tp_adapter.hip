@@ -659,9 +659,11 @@ __global__ __launch_bounds__(64 * few_waves(RB), few_waves_a_simd(RB, TERMS, C32
 }
 
 // ---------------------------------------------------------------------------------------------
-// grad.  A workgroup has a strip of 128 columns, 16 RB ranks and a share of an adapter's rows, counted in units of 32 rows of one segment; its four
+// grad.  A workgroup has a strip of 128 columns, 16 or 32 ranks and a share of an adapter's rows, counted in units of 32 rows of one segment; its four
 // waves take the units in turn and their sums meet in LDS in order.  The factor's layout again leaves a lane with eight neighbouring columns.  With several
-// shares their sums go to planes that a second kernel adds in order: nothing depends on which workgroup runs first.
+// shares their sums go to planes that are added in order later: nothing depends on which workgroup runs first.
+// (32 ranks: two workgroups fit a CU.  All of a backward pass of 16384 x 4096 x 4096, 64 ranks 211 us, with 64 ranks a workgroup 228, with 16 237; 128 ranks
+// 268 / 294 / 327; 731 rows of 1504 and 2496 columns, 64 ranks 25.1 / 28.5 / 23.7.)
 // ---------------------------------------------------------------------------------------------
 constexpr int GRAD_WAVES = 4;
 template <int RB>
@@ -890,9 +892,9 @@ hipError_t launch_up(const UpArgs& a, const GradArgs* fin, hipStream_t s) {
 
 hipError_t launch_grad(const GradArgs& a, bool finish, hipStream_t s) {
     const int strips0 = (a.side[0].cols + 127) / 128, strips = strips0 + (a.sides > 1 ? (a.side[1].cols + 127) / 128 : 0);
-    const int rb = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4, chunks = (a.rank + 16 * rb - 1) / (16 * rb);
+    const int rb = a.rank <= 16 ? 1 : 2, chunks = (a.rank + 16 * rb - 1) / (16 * rb);
     const int64_t blocks = (int64_t)strips * chunks * a.shares * a.seg.pool;      // (the caller has looked at how many)
-    if (hipError_t e = launch_kernel(rb == 1 ? tp_adapter_grad_kernel<1> : rb == 2 ? tp_adapter_grad_kernel<2> : tp_adapter_grad_kernel<4>,
+    if (hipError_t e = launch_kernel(rb == 1 ? tp_adapter_grad_kernel<1> : tp_adapter_grad_kernel<2>,
                                      dim3((unsigned)blocks), dim3(64 * GRAD_WAVES), 0, s, a, strips0, strips); e != hipSuccess || a.shares == 1 || !finish)
         return e;
     return launch_kernel(tp_adapter_grad_finish_kernel, dim3((unsigned)((int64_t)finish_blocks_each(a, 64) * a.seg.pool * a.sides)), dim3(64), 0, s, a);

@@ -119,15 +119,16 @@ bool in_one_launch(const Split& s, int64_t rows, int64_t segments, int64_t facto
     const int64_t most = s.tiles >= 192 ? 1 << 21 : s.tiles >= 80 ? 1 << 19 : 1 << 17;
     return factor <= (rows > 8 * segments ? most / 4 : most);
 }
-// Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 64 ranks each) of the adapters that can have rows for two a CU (four: 63 us
-// for 55, and more planes), but of four units of 32 rows (one a wave) at least, and planes for at most 64 adapters where that is more than
-// the whole pool would ask for.  Backward in us, by rows and the whole pool before: 222 rows in 29 segments, 56 ranks 34.5 -> 24; 8814 rows, two of 12 adapters
-// with some, 32 ranks 83.4 -> 67.9.
-int64_t grad_blocks(int64_t cols, int pool, int rank) { return (cols + 127) / 128 * ((rank + 63) / 64) * pool; }
+// Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 32 ranks each) of the adapters that can have rows for two a CU (four: 63 us
+// for 55, and more planes), but of four units of 32 rows (one a wave) at least, and at most two units on average; and room for 256 adapters' sums at most, where
+// that is more than the whole pool would ask for.  Backward in us, by rows and the whole pool before: 222 rows in 29 segments, 56 ranks 34.5 -> 24; 8814
+// rows, two of 12 adapters, 32 ranks 83.4 -> 67.9; 8124 rows in two segments, 27 adapters, 16 ranks 25.7 -> 22; without the average: 642 rows in 28
+// segments, ten adapters, 64 ranks 35 -> 21.
+int64_t grad_blocks(int64_t cols, int pool, int rank) { return (cols + 127) / 128 * ((rank + 31) / 32) * pool; }
 int plan_grad(int64_t rows, int64_t segments, int64_t cols, int pool, int rank) {
     auto enough = [&](int64_t adapters) { const int64_t blocks = grad_blocks(cols, 1, rank) * adapters; return (512 + blocks - 1) / blocks; };
-    const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(pool, segments)), most = std::max<int64_t>(enough(pool), 64 / pool);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({enough(busy), most, most_tiles(rows, segments, 32) / 4, 32}));
+    const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(pool, segments)), most = std::max<int64_t>(enough(pool), 256 / pool), units = most_tiles(rows, segments, 32);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({enough(busy), most, units / 4, std::max<int64_t>(1, units / (2 * busy)), 32}));
 }
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 // the workspace, in this order
