@@ -9,9 +9,9 @@
 // All three are bound by memory: the rank is at most 128, so a row of X or Y that is read takes 2 to 64 flops a byte.  V and U stay in fp32.  Where they
 // are a matrix operand they go in as a sum of bf16 terms, two (2^-17) for bf16 results and three (2^-25) for fp32 ones: the matrix
 // unit has the time, and rounding them once would cost a bf16 step of the adapters' part.
-// Measured (all of a call, us, and the bytes it cannot do without over that): one token of 4096 x 4096, 16 ranks 7.1; 96 tokens over 48 adapters 9.5; 5923
+// Measured (all of a call, us, and the bytes it cannot do without over that): one token of 4096 x 4096, 16 ranks 7.2; 96 tokens over 48 adapters 9.5; 5923
 // rows in 12 segments, 32 ranks, GeLU 56 (4.4 TB/s); 2048 x 4 x 2048 x 8192, 64 ranks, dropout 30 (3.5); backward of 16384 x 4096 x 4096, 16 ranks, dropout,
-// fp32 179 (4.5), of 32896 x 640 over 2 x 2560, 8 ranks 111 (4.2).  A large copy reaches 5.2 TB/s.
+// fp32 178 (4.5), of 32896 x 640 over 2 x 2560, 8 ranks 108 (4.3).  A large copy reaches 5.2 TB/s.
 //
 // Rows come in segments, a request each, described by device arrays.  A workgroup works on a tile of one segment's rows: it finds its tile from
 // the offsets itself (one trip to memory for up to 64 segments), so a call is the same launches whatever the lengths, and can be captured.  Offsets are
