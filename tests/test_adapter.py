@@ -714,3 +714,45 @@ def test_an_infinite_factor_stays_in_its_columns():
     hit = torch.zeros(m, n, dtype=torch.bool, device="cuda")
     hit[30:, 77] = True
     assert torch.equal(y[~hit], z[~hit]) and not torch.isfinite(z[hit]).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,pool,rank,cuts,ids", [(700, 7, 40, [0, 333, 690], [5, 2]), (900, 1, 128, [0, 1, 900], [0, 0]), (1500, 40, 16, [3, 1490], [39])])
+def test_gradients_are_the_same_with_and_without_dx(m, pool, rank, cuts, ids):
+    """The factors' gradients of a pool of which few adapters have rows, in shares: right, zeros elsewhere, the same bits whichever launch adds the shares up, and
+    added to what is there if that is asked for."""
+    h, n = 136, 264
+    g = _g(41)
+    grid, dims = T.Grid(T.MODE_1D_COL), (m, h, n)
+    x, a, b, c, dy = _strided(g, m, h), _strided(g, pool, rank, h), _strided(g, pool, rank, n), _strided(g, m, h), _strided(g, m, n)
+    ad = T.Adapters(torch.tensor(cuts, dtype=torch.int32, device="cuda"), torch.tensor(ids, dtype=torch.int32, device="cuda"), pool, rank)
+    ws = torch.empty(T.tp_adapter_workspace_size(grid, dims, T.PASS_DX, ad), dtype=torch.uint8, device="cuda")
+    v = torch.randn(m, rank, generator=g, device="cuda")
+    dx = torch.full((m, h), 7.0, device="cuda")
+
+    def grads(with_dx, start=None):
+        da, db = (torch.full((pool, rank, k), float("nan"), device="cuda") if start is None else start[i].clone() for i, k in enumerate((h, n)))
+        T.tp_adapter_bwd(grid, dims, 1, ad, [dy], [b], a=a if with_dx else None, dx_base=c if with_dx else None, dx=dx if with_dx else None, x_own=x, da=da, dy_own=dy, v=v, db=db,
+                         accumulate=start is not None, workspace=ws)
+        return da, db
+
+    one, two = grads(True), grads(False)
+    for p, q in zip(one, two):
+        assert torch.equal(p, q)
+    start = [torch.randn(t.shape, generator=g, device="cuda") for t in one]
+    for p, q, s, t in zip(grads(True, start), grads(False, start), start, one):
+        assert torch.equal(p, q) and torch.equal(p, s + t)
+    # against 64 bits: U and the terms of both sums are off by what fp32 sums of K products and of a segment's rows are
+    d64 = lambda t: t.double()
+    want = [torch.zeros(t.shape, dtype=torch.float64, device="cuda") for t in one]
+    size = [torch.zeros(t.shape, dtype=torch.float64, device="cuda") for t in one]
+    for lo, hi, i in zip(cuts, cuts[1:], ids):
+        u, mu = d64(dy[lo:hi]) @ d64(b[i]).t().contiguous(), d64(dy[lo:hi]).abs() @ d64(b[i]).abs().t().contiguous()
+        want[0][i] += u.t().contiguous() @ d64(x[lo:hi])
+        size[0][i] += mu.t().contiguous() @ d64(x[lo:hi]).abs()
+        want[1][i] += d64(v[lo:hi]).t().contiguous() @ d64(dy[lo:hi])
+        size[1][i] += d64(v[lo:hi]).abs().t().contiguous() @ d64(dy[lo:hi]).abs()
+    for got, w, s in zip(one, want, size):
+        assert ((got.double() - w).abs() <= (m + n + 16) * E24 * s).all()
+        idle = [i for i in range(pool) if i not in ids]
+        assert (got[idle] == 0).all()
