@@ -222,7 +222,7 @@ def _call():
     names = ("tp_linear_fwd_ex", "tp_linear_fwd_static", "tp_linear_bwd_ex", "tp_linear_bwd_partials_ex", "tp_bias_act", "tp_dgelu",
              "tp_bias_grad")
     m.bind(*[C.cast(getattr(L, n), C.c_void_p).value for n in names], *dtypes)
-    ops = ("tp_dropout_fwd", "tp_dropout_bwd", "tp_adapter_fwd", "tp_adapter_bwd")
+    ops = ("tp_dropout_fwd", "tp_dropout_bwd", "tp_adapter_fwd", "tp_adapter_bwd", "tp_block_map")
     m.bind_ops(*[C.cast(getattr(L, n), C.c_void_p).value for n in ops], *more, device)
     return m
 

@@ -22,6 +22,7 @@ PyObject* g_tensor;                                                             
 PyObject *g_i32, *g_f32, *g_bf16;                                                            // torch.int32, torch.float32, torch.bfloat16
 PyObject *g_current_device;                                                          // callable, or None: its answer is not compared
 
+decltype(&tp_block_map) f_block_map;
 decltype(&tp_linear_fwd_ex) f_fwd;
 decltype(&tp_linear_fwd_static) f_static;
 decltype(&tp_linear_bwd_ex) f_bwd;
@@ -296,8 +297,8 @@ PyObject* bias_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return nullptr;
     return answer([&] { return f_bias_grad(da.ptr, da.ld, rows, cols, db, ws.ptr, ws.bytes, stream); });
 }
-// The calls below also look at what the C functions cannot see of a tensor: its type, where only one fits, and that all of a call's
-// tensors are on the current device (a kernel that follows a host address ends the process).
+// The calls below also look at what the C functions cannot see of a tensor: its type, where only one fits, that it holds all that the call's extents
+// say (a kernel goes by those), and that all of a call's tensors are on the current device (a kernel that follows a host address ends the process).
 struct Devices {
     int64_t seen = -1;
     bool add(PyObject* t) {
@@ -351,8 +352,34 @@ bool flat(PyObject* t, int64_t want, const char* what) {
 // a bias or its gradient
 bool to_flat(PyObject* o, PyObject* type, Devices* at, int64_t want, const char* what, void** p) { return look(o, type, at) && flat(o, want, what) && to_ptr(o, p); }
 
+// What a tensor has to hold; nothing with no rows or columns (of what the call does not use, or the library refuses)
+struct Extents { int64_t rows = 0, cols = 0; const char* what = ""; };
+bool holds(const Extents& e, int64_t rows, int64_t cols) {
+    if (e.rows <= 0 || e.cols <= 0 || (rows >= e.rows && cols >= e.cols)) return true;
+    PyErr_Format(PyExc_ValueError, "%s must have at least %lld rows of %lld columns, got %lld of %lld", e.what, (long long)e.rows, (long long)e.cols,
+                 (long long)rows, (long long)cols);
+    return false;
+}
+// the leading dimension of a tensor as tensor_ld() takes it, with these extents
+bool tensor_ld(PyObject* t, const Extents& e, int64_t* ld) {
+    Ref st(PyObject_CallMethodNoArgs(t, s_stride)), sh(PyObject_GetAttr(t, s_shape));
+    if (!st || !sh) return false;
+    const Py_ssize_t n = PySequence_Size(st.p);
+    if (n < 0) return false;
+    int64_t rows = 1, cols, unit;
+    if (n == 2) {
+        if (!item(sh.p, 0, &rows) || !item(sh.p, 1, &cols) || !item(st.p, 0, ld) || !item(st.p, 1, &unit)) return false;
+        if (unit == 1 || cols <= 1) return holds(e, rows, cols);
+    } else if (n == 1) {
+        if (!item(sh.p, 0, &cols) || !item(st.p, 0, &unit)) return false;
+        *ld = cols;
+        if (unit == 1 || cols <= 1) return holds(e, rows, cols);
+    }
+    PyErr_SetString(PyExc_ValueError, "blocks must be 2-D with unit column stride");
+    return false;
+}
 // A block: None, a sequence as to_oblk() and to_cblk() take it, or a tensor on the current device of type `want` (null: fp32 or bf16, else 99)
-bool to_block(PyObject* o, PyObject* want, Devices* at, tp_oblk_t* b) {
+bool to_block(PyObject* o, PyObject* want, Devices* at, const Extents& e, tp_oblk_t* b) {
     bool tensor = false;
     if (o == Py_None) return to_oblk(o, b);
     if (!is_tensor(o, &tensor)) return false;
@@ -364,7 +391,7 @@ bool to_block(PyObject* o, PyObject* want, Devices* at, tp_oblk_t* b) {
         return true;
     }
     int64_t ptr = 0, ld = 0;
-    if (!at->add(o) || !call0(o, s_data_ptr, &ptr) || !tensor_ld(o, &ld)) return false;
+    if (!at->add(o) || !call0(o, s_data_ptr, &ptr) || !tensor_ld(o, e, &ld)) return false;
     Ref dt(PyObject_GetAttr(o, s_dtype));
     if (!dt) return false;
     if (want && want != Py_None && dt.p != want) {
@@ -374,16 +401,16 @@ bool to_block(PyObject* o, PyObject* want, Devices* at, tp_oblk_t* b) {
     *b = tp_oblk_t{reinterpret_cast<void*>(ptr), ld, dt.p == g_f32 ? TP_F32 : dt.p == g_bf16 ? TP_BF16 : 99};
     return true;
 }
-bool to_input(PyObject* o, Devices* at, tp_cblk_t* b) {           // bf16
+bool to_input(PyObject* o, Devices* at, const Extents& e, tp_cblk_t* b) {           // bf16
     tp_oblk_t q;
-    if (!to_block(o, g_bf16, at, &q)) return false;
+    if (!to_block(o, g_bf16, at, e, &q)) return false;
     *b = tp_cblk_t{q.ptr, q.ld};
     return true;
 }
 struct Inputs {                                                  // a list of them, with empty ones up to TP_MAX_STEPS; None: a null pointer
     tp_cblk_t blocks[TP_MAX_STEPS] = {};
     const tp_cblk_t* ptr = nullptr;
-    bool fill(PyObject* o, Devices* at) {
+    bool fill(PyObject* o, Devices* at, const Extents& e, int used) {      // (the first `used` are read)
         if (o == Py_None) return true;
         if (PyObject_Size(o) < 0) return false;
         Ref s(PySequence_Fast(o, "blocks must be a sequence"));
@@ -391,7 +418,7 @@ struct Inputs {                                                  // a list of th
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(s.p);
         if (n > TP_MAX_STEPS) { PyErr_SetString(PyExc_ValueError, "too many blocks"); return false; }
         for (Py_ssize_t i = 0; i < n; ++i)
-            if (!to_input(PySequence_Fast_GET_ITEM(s.p, i), at, blocks + i)) return false;
+            if (!to_input(PySequence_Fast_GET_ITEM(s.p, i), at, i < used ? e : Extents{}, blocks + i)) return false;
         ptr = blocks;
         return true;
     }
@@ -399,9 +426,9 @@ struct Inputs {                                                  // a list of th
 struct MaybeInput {
     tp_cblk_t b;
     const tp_cblk_t* ptr = nullptr;
-    bool fill(PyObject* o, Devices* at) {
+    bool fill(PyObject* o, Devices* at, const Extents& e) {
         if (o == Py_None) return true;
-        if (!to_input(o, at, &b)) return false;
+        if (!to_input(o, at, e, &b)) return false;
         ptr = &b;
         return true;
     }
@@ -437,9 +464,9 @@ bool to_dropout(PyObject* o, tp_dropout_t* d, Devices* at) {
 // dropout_fwd(dropout, x, bias, epi, residual, y, preact, rows, cols, stream)
 PyObject* dropout_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     tp_dropout_t d; tp_oblk_t x, y, pre; tp_cblk_t res; void *bias, *stream; int epi; int64_t rows, cols; Devices at;
-    if (!count(n, 10) || !to_dropout(a[0], &d, &at) || !to_block(a[1], nullptr, &at, &x) || !to_i64(a[7], &rows) || !to_i64(a[8], &cols) ||
-        !to_flat(a[2], g_bf16, &at, cols, "bias", &bias) || !to_int(a[3], &epi) || !to_input(a[4], &at, &res) || !to_block(a[5], nullptr, &at, &y) ||
-        !to_block(a[6], nullptr, &at, &pre) || !to_ptr(a[9], &stream))
+    if (!count(n, 10) || !to_i64(a[7], &rows) || !to_i64(a[8], &cols) || !to_dropout(a[0], &d, &at) || !to_block(a[1], nullptr, &at, {rows, cols, "x"}, &x) ||
+        !to_flat(a[2], g_bf16, &at, cols, "bias", &bias) || !to_int(a[3], &epi) || !to_input(a[4], &at, {rows, cols, "residual"}, &res) ||
+        !to_block(a[5], nullptr, &at, {rows, cols, "y"}, &y) || !to_block(a[6], nullptr, &at, {rows, cols, "preact"}, &pre) || !to_ptr(a[9], &stream))
         return nullptr;
     return answer([&] { return f_dropout_fwd(&d, x.ptr, x.ld, x.dtype, bias, epi, res, y, pre, rows, cols, stream); });
 }
@@ -447,7 +474,8 @@ PyObject* dropout_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* dropout_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     tp_dropout_t d; tp_cblk_t dy, pre, dx; void *db, *stream; int64_t rows, cols; Workspace ws; Devices at;
     if (!count(n, 9) || !to_i64(a[5], &rows) || !to_i64(a[6], &cols) || !to_flat(a[4], g_f32, &at, cols, "db", &db) || !look(a[7], nullptr, &at) ||
-        !to_dropout(a[0], &d, &at) || !to_input(a[1], &at, &dy) || !to_input(a[2], &at, &pre) || !to_input(a[3], &at, &dx) || !to_ws(a[7], &ws) || !to_ptr(a[8], &stream))
+        !to_dropout(a[0], &d, &at) || !to_input(a[1], &at, {rows, cols, "dy"}, &dy) || !to_input(a[2], &at, {rows, cols, "preact"}, &pre) ||
+        !to_input(a[3], &at, {rows, cols, "dx"}, &dx) || !to_ws(a[7], &ws) || !to_ptr(a[8], &stream))
         return nullptr;
     return answer([&] {
         return f_dropout_bwd(&d, dy.ptr, dy.ld, pre.ptr, pre.ld, const_cast<void*>(dx.ptr), dx.ld, db, rows, cols, ws.ptr, ws.bytes, stream);
@@ -475,7 +503,7 @@ bool to_adapters(PyObject* o, tp_adapters_t* a, Devices* at) {
     return true;
 }
 // A factor: a tensor [n_adapters, rank, cols] with unit column stride, (address, leading dimension, stride) or None
-template <class F> bool to_factor(PyObject* o, F* f, const tp_adapters_t& a, PyObject* type, Devices* at) {
+template <class F> bool to_factor(PyObject* o, F* f, const tp_adapters_t& a, PyObject* type, Devices* at, int64_t cols, const char* what) {
     int64_t ptr = 0, ld = 0, stride = 0;
     if (o != Py_None) {
         bool tensor;
@@ -486,13 +514,18 @@ template <class F> bool to_factor(PyObject* o, F* f, const tp_adapters_t& a, PyO
             if (!look(o, type, at) || !call0(o, s_data_ptr, &ptr)) return false;
             Ref st(PyObject_CallMethodNoArgs(o, s_stride)), sh(PyObject_GetAttr(o, s_shape));
             if (!st || !sh) return false;
-            int64_t n, r, unit;
-            if (PySequence_Size(st.p) != 3 || !item(sh.p, 0, &n) || !item(sh.p, 1, &r) || !item(st.p, 0, &stride) || !item(st.p, 1, &ld) || !item(st.p, 2, &unit)) {
+            int64_t n, r, have, unit;
+            if (PySequence_Size(st.p) != 3 || !item(sh.p, 0, &n) || !item(sh.p, 1, &r) || !item(sh.p, 2, &have) ||
+                !item(st.p, 0, &stride) || !item(st.p, 1, &ld) || !item(st.p, 2, &unit)) {
                 if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a factor must be [n_adapters, rank, cols]");
                 return false;
             }
             if (n != a.n_adapters || r != a.rank || unit != 1) {
                 PyErr_SetString(PyExc_ValueError, "a factor must be [n_adapters, rank, cols] with unit column stride");
+                return false;
+            }
+            if (have < cols) {
+                PyErr_Format(PyExc_ValueError, "%s must have at least %lld columns, got %lld", what, (long long)cols, (long long)have);
                 return false;
             }
             if (n == 1) stride = 0;                                      // (never used; torch puts anything there)
@@ -506,7 +539,7 @@ template <class F> bool to_factor(PyObject* o, F* f, const tp_adapters_t& a, PyO
 struct Factors {
     tp_factor_t at_[TP_MAX_STEPS] = {};
     const tp_factor_t* ptr = nullptr;
-    bool fill(PyObject* o, const tp_adapters_t& a, Devices* at) {
+    bool fill(PyObject* o, const tp_adapters_t& a, Devices* at, int64_t cols, const char* what, int used) {
         if (o == Py_None) return true;
         if (PyObject_Size(o) < 0) return false;
         Ref s(PySequence_Fast(o, "factors must be a sequence"));
@@ -514,15 +547,15 @@ struct Factors {
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(s.p);
         if (n > TP_MAX_STEPS) { PyErr_SetString(PyExc_ValueError, "too many factors"); return false; }
         for (Py_ssize_t i = 0; i < n; ++i)
-            if (!to_factor(PySequence_Fast_GET_ITEM(s.p, i), at_ + i, a, g_bf16, at)) return false;
+            if (!to_factor(PySequence_Fast_GET_ITEM(s.p, i), at_ + i, a, g_bf16, at, i < used ? cols : 0, what)) return false;
         ptr = at_;
         return true;
     }
 };
 // V: fp32 [rows, rank], one row behind the other
-bool to_v(PyObject* o, float** v, Devices* at) {
+bool to_v(PyObject* o, float** v, Devices* at, int64_t rows, int rank) {
     void* p;
-    if (!to_flat(o, g_f32, at, 0, "v", &p)) return false;
+    if (!to_flat(o, g_f32, at, rank > 0 ? rows * rank : 0, "v", &p)) return false;
     *v = static_cast<float*>(p);
     return true;
 }
@@ -536,14 +569,25 @@ struct MaybeDropout {
         return true;
     }
 };
+// Extents of the rank's share in one pass; zeros where the library will refuse it
+struct Share { int64_t m = 0, n = 0, k = 0; };
+Share share(const tp_grid_t* grid, const tp_dims_t* dims, int pass) {
+    Share s;
+    if (f_block_map(grid, dims, pass, nullptr, &s.m, &s.n, &s.k, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr) != TP_OK ||
+        s.m > INT32_MAX || s.n > INT32_MAX || s.k > INT32_MAX)
+        return Share{};
+    return s;
+}
 // adapter_fwd(grid, dims, n_steps, adapters, x_blocks, a_blocks, b, dropout, c, bias, epi, y, preact, v, workspace, stream)
 PyObject* adapter_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const tp_grid_t* grid; tp_dims_t dims; int steps, epi; tp_adapters_t ad; Inputs x; Factors f; tp_factor_t b; MaybeDropout drop; tp_oblk_t c, y, pre;
     void *bias, *stream; float* v; Workspace ws; Devices at;
-    if (!count(n, 16) || !to_struct(a[0], &grid) || !to_dims(a[1], &dims) || !to_int(a[2], &steps) || !to_adapters(a[3], &ad, &at) ||
-        !x.fill(a[4], &at) || !f.fill(a[5], ad, &at) || !to_factor(a[6], &b, ad, g_bf16, &at) || !drop.fill(a[7], &at) ||
-        !to_block(a[8], nullptr, &at, &c) || !to_flat(a[9], g_bf16, &at, 0, "bias", &bias) || !to_int(a[10], &epi) ||
-        !to_block(a[11], nullptr, &at, &y) || !to_block(a[12], nullptr, &at, &pre) || !to_v(a[13], &v, &at) ||
+    if (!count(n, 16) || !to_struct(a[0], &grid) || !to_dims(a[1], &dims) || !to_int(a[2], &steps) || !to_adapters(a[3], &ad, &at)) return nullptr;
+    const Share s = share(grid, &dims, TP_PASS_FWD);
+    if (!x.fill(a[4], &at, {s.m, s.k, "a block of X"}, steps) || !f.fill(a[5], ad, &at, s.k, "a chunk of A", steps) ||
+        !to_factor(a[6], &b, ad, g_bf16, &at, s.n, "b") || !drop.fill(a[7], &at) || !to_block(a[8], nullptr, &at, {s.m, s.n, "c"}, &c) ||
+        !to_int(a[10], &epi) || !to_flat(a[9], g_bf16, &at, epi == TP_EPI_NONE ? 0 : s.n, "bias", &bias) ||
+        !to_block(a[11], nullptr, &at, {s.m, s.n, "y"}, &y) || !to_block(a[12], nullptr, &at, {s.m, s.n, "preact"}, &pre) || !to_v(a[13], &v, &at, s.m, ad.rank) ||
         !look(a[14], nullptr, &at) || !to_ws(a[14], &ws) || !to_ptr(a[15], &stream))
         return nullptr;
     return answer([&] {
@@ -554,11 +598,16 @@ PyObject* adapter_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* adapter_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const tp_grid_t* grid; tp_dims_t dims; int steps, accumulate; tp_adapters_t ad; Inputs dy; Factors f; tp_factor_t fa; MaybeDropout drop;
     tp_oblk_t base, dx; MaybeInput x, own; tp_factor_out_t da, db; float* v; void* stream; Workspace ws; Devices at;
-    if (!count(n, 18) || !to_struct(a[0], &grid) || !to_dims(a[1], &dims) || !to_int(a[2], &steps) || !to_adapters(a[3], &ad, &at) ||
-        !dy.fill(a[4], &at) || !f.fill(a[5], ad, &at) || !to_factor(a[6], &fa, ad, g_bf16, &at) || !drop.fill(a[7], &at) ||
-        !to_block(a[8], nullptr, &at, &base) || !to_block(a[9], nullptr, &at, &dx) || !x.fill(a[10], &at) ||
-        !to_factor(a[11], &da, ad, g_f32, &at) || !own.fill(a[12], &at) || !to_v(a[13], &v, &at) ||
-        !to_factor(a[14], &db, ad, g_f32, &at) || !to_int(a[15], &accumulate) || !look(a[16], nullptr, &at) || !to_ws(a[16], &ws) || !to_ptr(a[17], &stream))
+    if (!count(n, 18) || !to_struct(a[0], &grid) || !to_dims(a[1], &dims) || !to_int(a[2], &steps) || !to_adapters(a[3], &ad, &at)) return nullptr;
+    const Share s = share(grid, &dims, TP_PASS_DX), fs = share(grid, &dims, TP_PASS_FWD);
+    const bool wants_dx = a[9] != Py_None, wants_da = a[11] != Py_None, wants_db = a[14] != Py_None;       // (what is not used may be any block)
+    const int used = wants_dx || wants_da ? steps : 0;
+    if (!dy.fill(a[4], &at, {s.m, s.k, "a block of dY"}, used) || !f.fill(a[5], ad, &at, s.k, "a chunk of B", used) ||
+        !to_factor(a[6], &fa, ad, g_bf16, &at, wants_dx ? s.n : 0, "a") || !drop.fill(a[7], &at) ||
+        !to_block(a[8], nullptr, &at, {wants_dx ? s.m : 0, s.n, "dx_base"}, &base) || !to_block(a[9], nullptr, &at, {s.m, s.n, "dx"}, &dx) ||
+        !x.fill(a[10], &at, {wants_da ? s.m : 0, s.n, "x_own"}) || !to_factor(a[11], &da, ad, g_f32, &at, s.n, "da") ||
+        !own.fill(a[12], &at, {wants_db ? fs.m : 0, fs.n, "dy_own"}) || !to_v(a[13], &v, &at, wants_db ? fs.m : 0, ad.rank) ||
+        !to_factor(a[14], &db, ad, g_f32, &at, fs.n, "db") || !to_int(a[15], &accumulate) || !look(a[16], nullptr, &at) || !to_ws(a[16], &ws) || !to_ptr(a[17], &stream))
         return nullptr;
     return answer([&] {
         return f_adapter_bwd(grid, &dims, steps, &ad, dy.ptr, f.ptr, a[6] == Py_None ? nullptr : &fa, drop.ptr, base, dx, x.ptr, da, own.ptr, v, db, accumulate,
@@ -583,15 +632,16 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-// bind_ops(addresses of the functions behind those, torch.int32, torch.Tensor, a function that gives the current device or None)
+// bind_ops(addresses of the functions behind those and of tp_block_map, torch.int32, torch.Tensor, a function that gives the current device or None)
 PyObject* bind_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    void* f[4];
-    if (!count(n, 7)) return nullptr;
-    for (int i = 0; i < 4; ++i)
+    void* f[5];
+    if (!count(n, 8)) return nullptr;
+    for (int i = 0; i < 5; ++i)
         if (!to_ptr(a[i], &f[i])) return nullptr;
-    Py_INCREF(a[4]); Py_XSETREF(g_i32, a[4]);
-    Py_INCREF(a[5]); Py_XSETREF(g_tensor, a[5]);
-    Py_INCREF(a[6]); Py_XSETREF(g_current_device, a[6]);
+    Py_INCREF(a[5]); Py_XSETREF(g_i32, a[5]);
+    Py_INCREF(a[6]); Py_XSETREF(g_tensor, a[6]);
+    Py_INCREF(a[7]); Py_XSETREF(g_current_device, a[7]);
+    f_block_map = reinterpret_cast<decltype(f_block_map)>(f[4]);
     f_adapter_fwd = reinterpret_cast<decltype(f_adapter_fwd)>(f[2]);
     f_adapter_bwd = reinterpret_cast<decltype(f_adapter_bwd)>(f[3]);
     f_dropout_fwd = reinterpret_cast<decltype(f_dropout_fwd)>(f[0]);

@@ -1,0 +1,142 @@
+"""What the calls of dropout and adapters refuse of their tensors, and what they take, seen on the host: stand-ins for tensors on the device whose addresses are
+never followed (every call that gets past the arguments is turned down by the library for its workspace or probability)."""
+import pytest
+import torch
+
+import paper_2110_14883_amd as T
+from paper_2110_14883_amd import binding as B
+
+BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+class Block:
+    """A tensor of device 0 as the binding sees one."""
+    def __init__(self, *shape, dtype=BF, stride=None, at=0x100000):
+        self.shape, self.dtype, self.at = shape, dtype, at
+        dense = [1] * len(shape)
+        for i in range(len(shape) - 2, -1, -1):
+            dense[i] = dense[i + 1] * max(1, shape[i + 1])
+        self.dense, self.strides = tuple(dense), tuple(stride or dense)
+
+    def data_ptr(self):
+        return self.at
+
+    def stride(self):
+        return self.strides
+
+    def numel(self):
+        return int(torch.Size(self.shape).numel())
+
+    def element_size(self):
+        return torch.empty(0, dtype=self.dtype).element_size()
+
+    def get_device(self):
+        return 0
+
+    def is_contiguous(self):
+        return self.strides == self.dense
+
+
+@pytest.fixture
+def device0(monkeypatch):
+    """The binding with device 0 as the current one."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    B._call.cache_clear()
+    B._call()
+    yield
+    monkeypatch.undo()
+    B._call.cache_clear()
+    B._call()
+
+
+def status(call):
+    with pytest.raises(T.TpError) as e:
+        call()
+    return e.value.status
+
+
+M, H, F, RANK = 48, 64, 136, 16
+GRID, DIMS = T.Grid(T.MODE_1D_COL), (M, H, F)
+AD = T.Adapters(Block(4, dtype=I32), Block(3, dtype=I32), 2, RANK, Block(2, dtype=F32))
+
+
+def fwd(epi=T.EPI_BIAS_GELU, grid=GRID, dims=DIMS, steps=1, ws=None, **k):
+    get = lambda name, *shape, **kw: k.get(name, Block(*shape, **kw))
+    T.tp_adapter_fwd(grid, dims, steps, k.get("ad", AD), k.get("xs") or [get("x", M, H)], k.get("as_") or [get("a", 2, RANK, H)], get("b", 2, RANK, F), get("c", M, F, at=0x200000),
+                     get("bias", F), epi, get("y", M, F, at=0x300000), preact=get("pre", M, F, at=0x400000), v=get("v", M, RANK, dtype=F32), workspace=ws, stream=0)
+
+
+def bwd(**k):
+    get = lambda name, *shape, **kw: k[name] if name in k else Block(*shape, **kw)
+    T.tp_adapter_bwd(GRID, DIMS, 1, AD, [get("dy", M, F)], [get("bs", 2, RANK, F)], a=get("a", 2, RANK, H), dx_base=get("base", M, H, at=0x200000), dx=get("dx", M, H, at=0x300000),
+                     x_own=get("x", M, H), da=get("da", 2, RANK, H, dtype=F32), dy_own=get("own", M, F), v=get("v", M, RANK, dtype=F32), db=get("db", 2, RANK, F, dtype=F32),
+                     workspace=None, stream=0)
+
+
+def test_adapters_take_blocks_that_hold_their_extents(device0):
+    """Exactly as large, larger, and cut out of a larger one: the workspace is what is missing then."""
+    assert status(fwd) == 7 and status(bwd) == 7
+    big = dict(x=Block(M + 1, H, stride=(H + 8, 1)), a=Block(2, RANK, H + 8), b=Block(2, RANK, F, stride=(4096, 256, 1)), bias=Block(F + 8), v=Block(M + 5, RANK, dtype=F32))
+    assert status(lambda: fwd(**big)) == 7
+    assert status(lambda: bwd(x=big["x"], a=big["a"], v=big["v"], db=Block(2, RANK, F + 8, dtype=F32))) == 7
+    assert status(lambda: fwd(v=Block(M * RANK, dtype=F32))) == 7 and status(lambda: fwd(epi=T.EPI_NONE, bias=Block(8))) == 7
+    # what is not used may be anything
+    assert status(lambda: bwd(da=None, x=Block(1, 8))) == 7 and status(lambda: bwd(db=None, own=Block(1, 8), v=Block(1, RANK, dtype=F32))) == 7
+    assert status(lambda: bwd(dx=None, a=Block(2, RANK, 8), base=Block(1, 8))) == 7 and status(lambda: bwd(dx=None, da=None, dy=Block(1, 8), bs=Block(2, RANK, 8))) == 7
+    # a grid's steps: the first n_steps blocks are read
+    grid, dims = T.Grid(T.MODE_2D, q=2, ri=1), (2 * M, 2 * H, 2 * F)
+    assert status(lambda: fwd(grid=grid, dims=dims, xs=[Block(M, H), Block(1, 8)], as_=[Block(2, RANK, H), Block(2, RANK, 8)])) == 7
+    with pytest.raises(ValueError):
+        fwd(grid=grid, dims=dims, steps=2, xs=[Block(M, H), Block(1, 8)], as_=[Block(2, RANK, H)] * 2)
+    with pytest.raises(ValueError):
+        fwd(grid=grid, dims=dims, steps=2, xs=[Block(M, H)] * 2, as_=[Block(2, RANK, H), Block(2, RANK, 8)])
+
+
+@pytest.mark.parametrize("name,block", [
+    ("v", Block(M - 1, RANK, dtype=F32)), ("bias", Block(F - 8)), ("x", Block(M - 1, H)), ("x", Block(M, H - 8)), ("x", Block(H)), ("a", Block(2, RANK, H - 8)), ("b", Block(2, RANK, F - 8)),
+    ("c", Block(M - 1, F)), ("c", Block(M, F - 8)), ("y", Block(M, F - 8)), ("y", Block(M - 1, F)), ("pre", Block(M - 1, F)), ("pre", Block(M, F - 8))])
+def test_adapter_forward_refuses_shorter_tensors(device0, name, block):
+    with pytest.raises(ValueError):
+        fwd(**{name: block})
+
+
+@pytest.mark.parametrize("name,block", [
+    ("v", Block(M - 1, RANK, dtype=F32)), ("dy", Block(M - 1, F)), ("dy", Block(M, F - 8)), ("bs", Block(2, RANK, F - 8)), ("a", Block(2, RANK, H - 8)), ("base", Block(M - 1, H)),
+    ("base", Block(M, H - 8)), ("dx", Block(M, H - 8)), ("dx", Block(M - 1, H)), ("x", Block(M - 1, H)), ("x", Block(M, H - 8)), ("own", Block(M - 1, F)), ("own", Block(M, F - 8)),
+    ("da", Block(2, RANK, H - 8, dtype=F32)), ("db", Block(2, RANK, F - 8, dtype=F32))])
+def test_adapter_backward_refuses_shorter_tensors(device0, name, block):
+    with pytest.raises(ValueError):
+        bwd(**{name: block})
+
+
+NO = T.Dropout(2.0, 1)          # (refused by the library, behind the tensors)
+
+
+def dfwd(x=None, y=None, bias=None, res=None, pre=None, rows=None, cols=None):
+    T.tp_dropout_fwd(NO, x or Block(M, F, dtype=F32), bias or Block(F), T.EPI_BIAS, y or Block(M, F, at=0x200000), residual=res or Block(M, F, at=0x300000),
+                     preact=pre or Block(M, F, at=0x400000), rows=rows, cols=cols, stream=0)
+
+
+def dbwd(dy=None, dx=None, pre=None, rows=None, cols=None):
+    T.tp_dropout_bwd(NO, dy or Block(M, F), dx or Block(M, F, at=0x200000), preact=pre or Block(M, F, at=0x300000), db=Block(F, dtype=F32), rows=rows, cols=cols, stream=0)
+
+
+def test_dropout_takes_blocks_that_hold_their_extents(device0):
+    assert status(dfwd) == 2 and status(dbwd) == 2
+    assert status(lambda: dfwd(y=Block(M + 1, F, stride=(F + 8, 1)), res=Block(M, F + 16))) == 2
+    assert status(lambda: dfwd(x=Block(M + 3, F + 8), rows=M, cols=F)) == 2 and status(lambda: dbwd(dy=Block(M + 3, F + 8), rows=M, cols=F)) == 2
+    assert status(lambda: dfwd(x=Block(F), rows=1, cols=F)) == 2
+
+
+@pytest.mark.parametrize("call,name,block", [(dfwd, "y", Block(M - 1, F)), (dfwd, "y", Block(M, F - 8)), (dfwd, "res", Block(M - 1, F)), (dfwd, "res", Block(M, F - 8)), (dfwd, "pre", Block(M - 1, F)),
+                                             (dfwd, "pre", Block(M, F - 8)), (dbwd, "dx", Block(M - 1, F)), (dbwd, "dx", Block(M, F - 8)), (dbwd, "pre", Block(M - 1, F)), (dbwd, "pre", Block(M, F - 8)),
+                                             (dfwd, "y", Block(F))])
+def test_dropout_refuses_shorter_tensors(device0, call, name, block):
+    with pytest.raises(ValueError):
+        call(**{name: block})
+
+
+def test_more_rows_than_the_tensor_has_are_refused(device0):
+    for call in (lambda: dfwd(x=Block(M, F, dtype=F32), rows=M + 1, cols=F), lambda: dbwd(dy=Block(M, F), rows=M, cols=F + 8), lambda: dfwd(x=Block(2 * F, stride=(2,)), rows=1, cols=F)):
+        with pytest.raises(ValueError):
+            call()
