@@ -374,7 +374,7 @@ typedef struct { void* ptr; int64_t ld, stride; } tp_factor_out_t;
  *   drop     : dropout on the adapters' input, or NULL.  Positions are those in the full X [M, H] (the library adds the blocks' own), behind
  *              row0, col0.
  *   c, y     : [m, n], fp32 or bf16 each: the shared product (tp_linear_fwd with TP_EPI_NONE) and the output.  y may be c itself (same address, type and
- *              leading dimension), else the two must not overlap (TP_ERR_SHAPE).   bias, epi, preact: as in tp_linear_fwd.
+ *              leading dimension), else the two must not overlap (TP_ERR_SHAPE; rows equally far apart may lie between each other's, else the spans count).   bias, epi, preact: as in tp_linear_fwd.
  *   v        : optional fp32 [m, rank], rows rank apart: V, saved for backward (rows without an adapter are not written).
  *   workspace: >= tp_adapter_workspace_size(.., TP_PASS_FWD, ..) bytes, 16-byte aligned; one call's at a time.
  * Apart from y over c no output may overlap an input or another output.

@@ -2,6 +2,7 @@
 #pragma once
 #include <cstddef>
 #include <cstdint>
+#include <utility>
 
 #include "tp_linear.h"
 
@@ -37,5 +38,14 @@ inline Range span(const void* p, int64_t ld, int64_t rows, int64_t cols, int es)
     return Range{lo, lo + (uintptr_t)(((rows - 1) * ld + cols) * es)};
 }
 inline bool overlap(const Range& a, const Range& b) { return a.lo < b.hi && b.lo < a.hi; }
+// The same of two blocks of `rows` rows, row by row where their rows lie equally far apart: columns of one matrix may lie between each other's rows.
+// (pitch, width: bytes from row to row and of a row.)
+inline bool rows_overlap(const void* p, int64_t pitch, int64_t width, const void* q, int64_t pitch_q, int64_t width_q, int64_t rows) {
+    if (pitch != pitch_q) return overlap(span(p, pitch, rows, width, 1), span(q, pitch_q, rows, width_q, 1));
+    uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    if (b < a) { std::swap(a, b); std::swap(width, width_q); }
+    const uint64_t down = (uint64_t)(b - a) / (uint64_t)pitch, right = (uint64_t)(b - a) % (uint64_t)pitch;      // b's first row from a's, and its first byte there
+    return (down < (uint64_t)rows && right < (uint64_t)width) || (down + 1 < (uint64_t)rows && right + (uint64_t)width_q > (uint64_t)pitch);
+}
 
 }  // namespace tpl

@@ -60,8 +60,8 @@ int check_factor(const void* ptr, int64_t ld, int64_t stride, const tp_adapters_
 // an operand and the output over it: the same block or apart
 int check_over(const tp_oblk_t& c, const tp_oblk_t& y, int64_t rows, int64_t cols) {
     if (c.ptr == y.ptr && c.ld == y.ld && c.dtype == y.dtype) return TP_OK;
-    auto bytes = [&](const tp_oblk_t& b) { return span(b.ptr, b.ld, rows, cols, b.dtype == TP_F32 ? 4 : 2); };
-    return overlap(bytes(c), bytes(y)) ? TP_ERR_SHAPE : TP_OK;
+    const int64_t size = c.dtype == TP_F32 ? 4 : 2, size_y = y.dtype == TP_F32 ? 4 : 2;
+    return rows_overlap(c.ptr, c.ld * size, cols * size, y.ptr, y.ld * size_y, cols * size_y, rows) ? TP_ERR_SHAPE : TP_OK;
 }
 
 // Tiles of at most `tile` rows that segments over `rows` rows can have

@@ -140,3 +140,17 @@ def test_more_rows_than_the_tensor_has_are_refused(device0):
     for call in (lambda: dfwd(x=Block(M, F, dtype=F32), rows=M + 1, cols=F), lambda: dbwd(dy=Block(M, F), rows=M, cols=F + 8), lambda: dfwd(x=Block(2 * F, stride=(2,)), rows=1, cols=F)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("rows,pitch,wide", [(1, 256, 256), (5, 256, 256), (5, 512, 256), (5, 512, 384), (3, 1024, 256), (32, 512, 272)])
+def test_blocks_that_share_no_byte_may_lie_between_each_others_rows(rows, pitch, wide):
+    """Every distance of y from c, against the sets of their bytes: refused where they share one (but for c itself), else the workspace is what is missing."""
+    ld, cols, at = pitch // 2, wide // 2, 0x400000
+    c_bytes = {i * pitch + b for i in range(rows) for b in range(0, wide, 16)}
+    for d in range(-(rows + 1) * pitch, (rows + 1) * pitch + 1, 16):
+        shares = any(x + d in c_bytes for x in c_bytes)
+
+        def call():
+            T.tp_adapter_fwd(GRID, (rows, H, cols), 1, T.Adapters(0x100, 0x200, 2, RANK, None, 1), [(0x10000, H)], [(0x20000, H, RANK * H)], (0x30000, cols, RANK * cols),
+                             (at, ld, B.DT_BF16), None, T.EPI_NONE, (at + d, ld, B.DT_BF16), workspace=None, stream=0)
+        assert status(call) == (4 if shares and d else 7), d
