@@ -329,7 +329,8 @@ typedef struct { uint64_t seed, offset; const uint64_t* offset_dev; int64_t row0
  *     A = x + bias,   y = drop(GeLU(A)) + residual  (epi TP_EPI_BIAS_GELU; TP_EPI_BIAS: drop(A) + residual; TP_EPI_NONE: drop(x) + residual)
  *   x        : fp32 or bf16 (x_dtype) [rows, cols];  bias: bf16 [cols] or NULL with TP_EPI_NONE;
  *   residual : optional bf16 [rows, cols] (NULL ptr: none);  y: fp32 or bf16;  preact: optional bf16 copy of A.
- * y may be x or residual itself (same address, type and leading dimension).  cols and every ld multiples of 8.  HBM-bound.
+ * y, or preact, may be x or residual itself (same address, type and leading dimension); apart from that neither may overlap these or the other
+ * (TP_ERR_SHAPE; blocks whose rows lie equally far apart may lie between each other's rows, for others their spans count).  cols and every ld multiples of 8.  HBM-bound.
  * Defined by: Section 2.2, 1D paragraph and the chunk shapes of 2D / 2.5D / 3D, as tp_bias_act: what is applied to a rank's chunk of the output
  * once it exists.  Nothing is done with rows = 0 or cols = 0 (blocks may be NULL then).
  * Errors: TP_ERR_NULL, TP_ERR_MODE, TP_ERR_SHAPE, TP_ERR_ALIGN, TP_ERR_DTYPE, TP_ERR_HIP.
@@ -340,7 +341,7 @@ int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_
 /*
  * tp_dropout_bwd -- its gradient:  dx = drop'(dy) GeLU'(preact)  (without preact: drop'(dy)), bf16, and optionally db (fp32 [cols]): the
  * column sums of dx before its rounding, in an order fixed by (rows, cols) and whether there is a workspace.  The residual's gradient is dy itself.
- *   drop      : as in forward.   dy, preact, dx: bf16 [rows, cols];  dx may be dy itself.
+ *   drop      : as in forward.   dy, preact, dx: bf16 [rows, cols];  dx may be dy or preact itself (same leading dimension), else must not overlap it (TP_ERR_SHAPE).
  *   workspace : as in tp_bias_grad (tp_bias_grad_workspace_size(rows, cols) bytes, 16-byte aligned, or NULL); read only if db is wanted.
  * With rows = 0 db is all zeros (blocks may be NULL then).  Errors: as tp_dropout_fwd, and TP_ERR_WORKSPACE.
  */

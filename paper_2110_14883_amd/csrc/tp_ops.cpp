@@ -28,6 +28,13 @@ int check_dropout(const tp_dropout_t* d, int64_t row, int64_t col, int64_t rows,
     return TP_OK;
 }
 
+// Memory of a dropout call: a block's address, the bytes from row to row and of a row (no address: none)
+struct Bytes { const void* p; int64_t pitch, width; };
+Bytes bytes_of(const void* p, int64_t ld, int64_t cols, int dtype) { const int64_t size = dtype == TP_F32 ? 4 : 2; return Bytes{p, ld * size, cols * size}; }
+bool apart(const Bytes& a, const Bytes& b, int64_t rows) { return !a.p || !b.p || !rows_overlap(a.p, a.pitch, a.width, b.p, b.pitch, b.width, rows); }
+// An output and an input are one block, whose elements a thread reads before it writes them, or apart
+bool over_or_apart(const Bytes& out, const Bytes& in, int64_t rows) { return (out.p == in.p && out.pitch == in.pitch && out.width == in.width) || apart(out, in, rows); }
+
 // ---------------------------------------------------------------------------------------------
 // adapters
 // ---------------------------------------------------------------------------------------------
@@ -314,6 +321,11 @@ int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_
         if (!aligned16(residual.ptr) || (residual.ld & 7)) return TP_ERR_ALIGN;
         if (residual.ld < cols) return TP_ERR_SHAPE;
     }
+    const Bytes in[] = {bytes_of(x, ld_x, cols, x_dtype), bytes_of(residual.ptr, residual.ld, cols, TP_BF16)},
+                out[] = {bytes_of(y.ptr, y.ld, cols, y.dtype), bytes_of(preact.ptr, preact.ld, cols, TP_BF16)};
+    if (!apart(out[0], out[1], rows)) return TP_ERR_SHAPE;
+    for (const Bytes& o : out)
+        if (!over_or_apart(o, in[0], rows) || !over_or_apart(o, in[1], rows)) return TP_ERR_SHAPE;
     DropArgs a;
     if (int e = check_dropout(drop, 0, 0, rows, cols, &a)) return e;
     if (launch_dropout(a, x, ld_x, x_dtype == TP_F32, epi == TP_EPI_NONE ? nullptr : bias, epi == TP_EPI_BIAS_GELU, residual.ptr, residual.ld, y.ptr, y.ld,
@@ -334,6 +346,10 @@ int tp_dropout_bwd(const tp_dropout_t* drop, const void* dy, int64_t ld_dy, cons
     if (int e = check_dropout(drop, 0, 0, rows, cols, &a)) return e;
     if (db_f32 && workspace && (!aligned16(workspace) || workspace_bytes < colsum_ws_bytes(rows, cols))) return TP_ERR_WORKSPACE;
     if (cols == 0) return TP_OK;
+    if (rows > 0) {
+        const Bytes out = bytes_of(dx, ld_dx, cols, TP_BF16);
+        if (!over_or_apart(out, bytes_of(dy, ld_dy, cols, TP_BF16), rows) || !over_or_apart(out, bytes_of(preact, ld_pre, cols, TP_BF16), rows)) return TP_ERR_SHAPE;
+    }
     if (launch_dropout_bwd(a, dy, ld_dy, preact, ld_pre, dx, ld_dx, rows, cols, static_cast<float*>(db_f32), static_cast<float*>(workspace),
                            static_cast<hipStream_t>(hip_stream)) != hipSuccess)
         return TP_ERR_HIP;

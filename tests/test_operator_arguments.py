@@ -123,7 +123,7 @@ def dbwd(dy=None, dx=None, pre=None, rows=None, cols=None):
 
 def test_dropout_takes_blocks_that_hold_their_extents(device0):
     assert status(dfwd) == 2 and status(dbwd) == 2
-    assert status(lambda: dfwd(y=Block(M + 1, F, stride=(F + 8, 1)), res=Block(M, F + 16))) == 2
+    assert status(lambda: dfwd(y=Block(M + 1, F, stride=(F + 8, 1), at=0x500000), res=Block(M, F + 16, at=0x600000))) == 2
     assert status(lambda: dfwd(x=Block(M + 3, F + 8), rows=M, cols=F)) == 2 and status(lambda: dbwd(dy=Block(M + 3, F + 8), rows=M, cols=F)) == 2
     assert status(lambda: dfwd(x=Block(F), rows=1, cols=F)) == 2
 
@@ -154,3 +154,21 @@ def test_blocks_that_share_no_byte_may_lie_between_each_others_rows(rows, pitch,
             T.tp_adapter_fwd(GRID, (rows, H, cols), 1, T.Adapters(0x100, 0x200, 2, RANK, None, 1), [(0x10000, H)], [(0x20000, H, RANK * H)], (0x30000, cols, RANK * cols),
                              (at, ld, B.DT_BF16), None, T.EPI_NONE, (at + d, ld, B.DT_BF16), workspace=None, stream=0)
         assert status(call) == (4 if shares and d else 7), d
+
+
+def test_dropout_outputs_that_overlap_what_is_read_are_refused():
+    """x at 0x100000, 32 rows of 64 columns, bf16 or fp32; a probability that the library refuses behind this stands for a forward call that passes."""
+    rows, cols, at = 32, 64, 0x100000
+    bf, f32 = B.DT_BF16, B.DT_F32
+    f = lambda x, y, res=None, pre=None: status(lambda: T.tp_dropout_fwd(NO, x, None, T.EPI_NONE, y, residual=res, preact=pre, rows=rows, cols=cols, stream=0))
+    b = lambda dy, dx, pre=None: status(lambda: T.tp_dropout_bwd(T.Dropout(0.1, 1), dy, dx, preact=pre, rows=rows, cols=cols, stream=0))
+    far = (0x900000, cols, bf)
+    assert f((at, cols, f32), (at, cols, f32)) == 2 and f((at, cols, bf), (at, cols, bf)) == 2 and f((at, 72, bf), (at, 72, bf)) == 2          # in place
+    assert f((at, cols, f32), far, res=(0x900000, cols)) == 2 and f((at, cols, bf), far, pre=(at, cols, bf)) == 2 and f((at, cols, f32), far, res=(0x500000, cols), pre=(0x500000, cols, bf)) == 2
+    assert f((at, 128, bf), (at + 128, 128, bf), res=(at, 128)) == 2                                                                          # columns of one matrix
+    assert f((at, cols, f32), (at, cols, bf)) == 4 and f((at, cols, bf), (at, cols, f32)) == 4 and f((at, cols, f32), (at, 2 * cols, bf)) == 4  # other types, other strides
+    assert f((at, cols, bf), (at, 72, bf)) == 4 and f((at, cols, bf), (at + 16, cols, bf)) == 4 and f((at, cols, bf), (at - 128 * 31, cols, bf)) == 4 and f((at, cols, bf), (at + 128 * 31, cols, bf)) == 4
+    assert f((at, cols, bf), (at + 128 * 32, cols, bf)) == 2 and f((at, cols, bf), (at - 128 * 32, cols, bf)) == 2
+    assert f((at, cols, f32), far, res=(0x900000, 72)) == 4 and f((at, cols, f32), (0x900000, cols, f32), res=(0x900000, cols)) == 4
+    assert f((at, cols, f32), far, pre=far) == 4 and f((at, cols, f32), far, pre=(at, cols, bf)) == 4 and f((at, cols, f32), far, res=(0x500000, cols), pre=(0x500010, cols, bf)) == 4
+    assert b((at, cols), (at + 16, cols)) == 4 and b((at, cols), (at, 72)) == 4 and b((at, cols), (0x900000, cols), pre=(0x900080, cols)) == 4

@@ -1,0 +1,60 @@
+"""Dropout and adapters where values and blocks are unusual: blocks over and between one another, infinities beside padded ranks, values that bf16 cannot hold,
+adapters that no row uses, many segments."""
+import math
+
+import pytest
+import torch
+
+import paper_2110_14883_amd as T
+from test_adapter import BF, F32, _g, _strided
+from test_dropout import _mask, _rand, factor, near, slope64
+
+pytestmark = pytest.mark.gpu
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("db", [0, 1])
+def test_dropout_blocks_between_each_others_rows_and_over_preact(db):
+    """dy, preact and dx as columns of one matrix, and dx over preact itself."""
+    rows, cols, d = 70, 136, T.Dropout(0.4, 8, 9, row0=3, col0=16)
+    m = _rand(rows, 3 * cols, BF, 51)
+    dy, pre, dx = (m[:, i * cols:(i + 1) * cols] for i in range(3))
+    ref = torch.where(_mask(d, rows, cols), dy.double() * factor(d.p) * slope64(pre.double()), 0.0)
+    keep = dy.clone()
+    work = (3 * 2.0 ** -24 + 1e-6) * max(1.0, float(ref.abs().max()))
+    sums = torch.empty(cols, device="cuda") if db else None
+    T.tp_dropout_bwd(d, dy, dx, preact=pre, db=sums)
+    near(dx, ref, BF, work)
+    first = dx.clone()
+    T.tp_dropout_bwd(d, dy, pre, preact=pre, db=sums)
+    assert torch.equal(pre, first) and torch.equal(dx, first) and torch.equal(dy, keep)
+    x, y = m[:, :cols], m[:, 2 * cols:]
+    want = torch.where(_mask(d, rows, cols), x.double() * factor(d.p), 0.0) + pre.double()
+    T.tp_dropout_fwd(d, x, None, T.EPI_NONE, y, residual=pre, preact=x)
+    near(y, want, BF, 3 * 2.0 ** -24 * float(want.abs().max()))
+    assert torch.equal(x, keep) and torch.equal(pre, first)
+
+
+def test_adapter_blocks_between_each_others_rows():
+    """c and y, dx_base and dx as columns of one matrix: what blocks apart give."""
+    m, h, n, rank = 50, 64, 72, 16
+    g = _g(52)
+    grid, dims = T.Grid(T.MODE_1D_COL), (m, h, n)
+    x, a, b, dy = _strided(g, m, h), _strided(g, 1, rank, h), _strided(g, 1, rank, n), _strided(g, m, n)
+    ad = T.Adapters(i32([0, 20, m]), i32([0, -1]), 1, rank)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    for p in (0.0, 0.3):
+        drop = T.Dropout(p, 1) if p else None
+        both = _strided(g, m, 2 * n, pad=0)
+        c, y, z = both[:, :n], both[:, n:], torch.empty(m, n, dtype=BF, device="cuda")
+        T.tp_adapter_fwd(grid, dims, 1, ad, [x], [a], b, c.clone(), None, 0, z, dropout=drop, workspace=ws)
+        keep = c.clone()
+        T.tp_adapter_fwd(grid, dims, 1, ad, [x], [a], b, c, None, 0, y, dropout=drop, workspace=ws)
+        assert torch.equal(y, z) and torch.equal(c, keep)
+        base, dx, dz = both[:, n:n + h], both[:, :h], torch.empty(m, h, dtype=BF, device="cuda")
+        T.tp_adapter_bwd(grid, dims, 1, ad, [dy], [b], a=a, dx_base=base.clone(), dx=dz, dropout=drop, workspace=ws)
+        T.tp_adapter_bwd(grid, dims, 1, ad, [dy], [b], a=a, dx_base=base, dx=dx, dropout=drop, workspace=ws)
+        assert torch.equal(dx, dz) and torch.equal(base, z[:, :h])
