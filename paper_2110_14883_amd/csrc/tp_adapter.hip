@@ -630,11 +630,15 @@ __global__ __launch_bounds__(64 * few_waves(RB), few_waves_a_simd(RB, TERMS, C32
         __syncthreads();
         for (int i = threadIdx.x; i < t.rows * GP; i += 64 * Sh::WAVES) {
             const int r = i / GP, q = i % GP;
-            const f32x4_t a = waves_sum<Sh::PART, Sh::WAVES>(part, r, 2 * q), b = waves_sum<Sh::PART, Sh::WAVES>(part, r, 2 * q + 1);
-            if (p.v_out && blockIdx.y == 0 && 8 * q < p.rank) {
-                f32x4_t* const to = reinterpret_cast<f32x4_t*>(p.v_out + (int64_t)(t.row0 + r) * p.rank + 8 * q);
-                to[0] = a;
-                to[1] = b;
+            f32x4_t a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
+            if (8 * q < p.rank) {                                // (sums of zeros beyond it, but NaN where X is not finite)
+                a = waves_sum<Sh::PART, Sh::WAVES>(part, r, 2 * q);
+                b = waves_sum<Sh::PART, Sh::WAVES>(part, r, 2 * q + 1);
+                if (p.v_out && blockIdx.y == 0) {
+                    f32x4_t* const to = reinterpret_cast<f32x4_t*>(p.v_out + (int64_t)(t.row0 + r) * p.rank + 8 * q);
+                    to[0] = a;
+                    to[1] = b;
+                }
             }
             const float v[8] = {a[0] * scale, a[1] * scale, a[2] * scale, a[3] * scale, b[0] * scale, b[1] * scale, b[2] * scale, b[3] * scale};
             lay_terms<GP, TERMS>(low, r, q, v);

@@ -58,3 +58,30 @@ def test_adapter_blocks_between_each_others_rows():
         T.tp_adapter_bwd(grid, dims, 1, ad, [dy], [b], a=a, dx_base=base.clone(), dx=dz, dropout=drop, workspace=ws)
         T.tp_adapter_bwd(grid, dims, 1, ad, [dy], [b], a=a, dx_base=base, dx=dx, dropout=drop, workspace=ws)
         assert torch.equal(dx, dz) and torch.equal(base, z[:, :h])
+
+
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 64, 72, 128])
+@pytest.mark.parametrize("rows", [3, 80])           # one launch, two launches
+@pytest.mark.parametrize("y_type", [BF, F32])
+def test_an_infinite_input_is_infinite_and_no_nan_for_any_rank(rank, rows, y_type):
+    """Factors of one sign: an infinite element of X makes its row of Y infinite, whatever lies in the ranks that fill up a matrix operand; the others stay as they are."""
+    h, n = 64, 136
+    g = _g(60 + rank)
+    grid, dims = T.Grid(T.MODE_1D_COL), (rows, h, n)
+    x, a, b, c = _strided(g, rows, h), _strided(g, 1, rank, h).abs() + 0.125, _strided(g, 1, rank, n).abs() + 0.125, _strided(g, rows, n)
+    ad = T.Adapters(i32([0, rows]), i32([0]), 1, rank)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+
+    def forward(x):
+        y, v = torch.full((rows, n), 7.0, dtype=y_type, device="cuda"), torch.full((rows, rank), 7.0, device="cuda")
+        T.tp_adapter_fwd(grid, dims, 1, ad, [x], [a], b, c, None, 0, y, v=v, workspace=ws)
+        return y, v
+
+    good = forward(x)
+    inf = float("inf")
+    for value in (inf, -inf):
+        x2 = x.clone()
+        x2[1, 5] = value
+        bad = forward(x2)
+        for p, q in zip(good, bad):
+            assert (q[1] == value).all() and torch.equal(p[0], q[0]) and torch.equal(p[2:], q[2:])
