@@ -84,22 +84,19 @@ __device__ __forceinline__ bool find_tile(const SegArgs& s, int t, int T, Tile& 
     return false;
 }
 
-// 8 values -> their bf16 terms: v = t[0] + t[1] (+ t[2]); an infinity is its first term alone
-template <int N>
+// 8 values -> their bf16 terms: v = t[0] + t[1] (+ t[2]).  The first is held to bf16's finite range: from 2^128 - 2^119 on fp32 numbers would round to an
+// infinity there, and leave another of the other sign.  (So an infinity has bf16's largest value as its first term and itself as the second.)
+template <int N>       // 2, 3
 __device__ __forceinline__ void split_terms(const float (&v)[8], u32x4_t (&t)[N]) {
-    float r[8];
+    constexpr float TOP = 0x1.FEp127f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = v[i];
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            t[n][i] = pack_bf16(r[2 * i], r[2 * i + 1]);
-            if (n + 1 < N) {
-                const float a = r[2 * i] - bf16_lo(t[n][i]), b = r[2 * i + 1] - bf16_hi(t[n][i]);
-                r[2 * i] = a == a ? a : 0.0f;
-                r[2 * i + 1] = b == b ? b : 0.0f;
-            }
+    for (int i = 0; i < 4; ++i) {
+        t[0][i] = pack_bf16(__builtin_amdgcn_fmed3f(v[2 * i], -TOP, TOP), __builtin_amdgcn_fmed3f(v[2 * i + 1], -TOP, TOP));
+        const float a = v[2 * i] - bf16_lo(t[0][i]), b = v[2 * i + 1] - bf16_hi(t[0][i]);
+        t[1][i] = pack_bf16(a, b);
+        if constexpr (N == 3) {
+            const float c = a - bf16_lo(t[1][i]), d = b - bf16_hi(t[1][i]);
+            t[2][i] = pack_bf16(c == c ? c : 0.0f, d == d ? d : 0.0f);               // (infinity less infinity: nothing is left)
         }
     }
 }

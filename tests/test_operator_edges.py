@@ -85,3 +85,44 @@ def test_an_infinite_input_is_infinite_and_no_nan_for_any_rank(rank, rows, y_typ
         bad = forward(x2)
         for p, q in zip(good, bad):
             assert (q[1] == value).all() and torch.equal(p[0], q[0]) and torch.equal(p[2:], q[2:])
+
+
+# V's largest values: 2^128 - 2^118 is an fp32 number that would round to an infinite bf16.  Exact as a sum of these three, in any order
+TOP = [2.0 ** 128 - 2.0 ** 120, 2.0 ** 119, 2.0 ** 118]
+
+
+@pytest.mark.parametrize("rank,rows", [(16, 3), (16, 80), (72, 3), (72, 80)])
+@pytest.mark.parametrize("y_type", [BF, F32])
+def test_finite_values_beyond_bf16s_largest(rank, rows, y_type):
+    """V and U of 2^128 - 2^118 and its opposite times factors of 2^-100: Y, dX, dA and dB are finite and right to their type's rounding (the products are exact
+    in fp32 but for the sum over ranks: 2^-24 a rank, and 2^-17 for V as two terms)."""
+    h, n, tiny = 64, 72, 2.0 ** -100
+    grid, dims = T.Grid(T.MODE_1D_COL), (rows, h, n)
+    z = lambda *s, t=BF: torch.zeros(*s, dtype=t, device="cuda")
+    x, a, b, dy = z(rows, h), z(1, rank, h), torch.full((1, rank, n), tiny, dtype=BF, device="cuda"), z(rows, n)
+    a[:, :, :3] = 1
+    top = torch.tensor(TOP, dtype=torch.float64, device="cuda").to(BF)
+    x[0, :3], x[1, :3] = top, -top
+    v_top = sum(TOP)
+    ad = T.Adapters(i32([0, rows]), i32([0]), 1, rank)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    y, v = z(rows, n, t=y_type), z(rows, rank, t=F32)
+    T.tp_adapter_fwd(grid, dims, 1, ad, [x], [a], b, z(rows, n), None, 0, y, v=v, workspace=ws)
+    assert (v[0].double() == v_top).all() and (v[1].double() == -v_top).all() and (v[2:] == 0).all()
+    want = torch.zeros(rows, n, dtype=torch.float64, device="cuda")
+    want[0], want[1] = rank * v_top * tiny, -rank * v_top * tiny
+    off = torch.finfo(y_type).eps / 2 + rank * 2.0 ** -24 + (2.0 ** -17 if y_type == BF else 2.0 ** -24)
+    assert ((y.double() - want).abs() <= off * want.abs()).all()
+    # backward: U = dY B^T with factors of one, dX = U A, dA = U^T X, dB = V^T dY
+    one, small = z(1, rank, n), torch.full((1, rank, h), tiny, dtype=BF, device="cuda")
+    one[:, :, :3] = 1
+    dy[0, :3], dy[1, :3] = top, -top
+    xs, dys = torch.full((rows, h), tiny, dtype=BF, device="cuda"), torch.full((rows, n), tiny, dtype=BF, device="cuda")
+    xs[1], dys[1] = -tiny, -tiny
+    dx, da, db = z(rows, h, t=y_type), z(1, rank, h, t=F32), z(1, rank, n, t=F32)
+    T.tp_adapter_bwd(grid, dims, 1, ad, [dy], [one], a=small, dx_base=z(rows, h), dx=dx, x_own=xs, da=da, dy_own=dys, v=v, db=db, workspace=ws)
+    want = torch.zeros(rows, h, dtype=torch.float64, device="cuda")
+    want[0], want[1] = rank * v_top * tiny, -rank * v_top * tiny
+    assert ((dx.double() - want).abs() <= off * want.abs()).all()
+    for t in (da, db):
+        assert ((t.double() - 2 * v_top * tiny).abs() <= 2.0 ** -22 * 2 * v_top * tiny).all()
