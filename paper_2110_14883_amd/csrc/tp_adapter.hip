@@ -775,7 +775,8 @@ __global__ __launch_bounds__(64 * GRAD_WAVES) void tp_adapter_grad_kernel(const 
         }
         base += __builtin_amdgcn_readlane(sums, 63);
     }
-    const float scale = (p.scale ? p.scale[a] : 1.0f) * (q.dropped ? p.drop.factor : 1.0f);
+    // (without rows 0, whatever the scale: that of a place in the pool which is not taken may be anything)
+    const float scale = total ? (p.scale ? p.scale[a] : 1.0f) * (q.dropped ? p.drop.factor : 1.0f) : 0.0f;
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
         if (i) __syncthreads();

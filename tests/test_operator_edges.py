@@ -126,3 +126,25 @@ def test_finite_values_beyond_bf16s_largest(rank, rows, y_type):
     assert ((dx.double() - want).abs() <= off * want.abs()).all()
     for t in (da, db):
         assert ((t.double() - 2 * v_top * tiny).abs() <= 2.0 ** -22 * 2 * v_top * tiny).all()
+
+
+@pytest.mark.parametrize("m", [40, 1500])           # one share of an adapter's rows, several
+def test_scales_of_adapters_without_rows_do_not_matter(m):
+    """They may be anything, as in a pool that is not full: zeros as the factors' gradients, or what was there."""
+    h, n, rank = 64, 72, 16
+    g = _g(70)
+    grid, dims = T.Grid(T.MODE_1D_COL), (m, h, n)
+    x, a, b, dy = _strided(g, m, h), _strided(g, 4, rank, h), _strided(g, 4, rank, n), _strided(g, m, n)
+    v = torch.randn(m, rank, generator=g, device="cuda")
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+
+    def grads(scale, start):
+        ad = T.Adapters(i32([0, m // 2, m]), i32([1, -1]), 4, rank, torch.tensor(scale, device="cuda"))
+        da, db = (torch.full((4, rank, k), start, device="cuda") for k in (h, n))
+        T.tp_adapter_bwd(grid, dims, 1, ad, [dy], [b], x_own=x, da=da, dy_own=dy, v=v, db=db, accumulate=start != 7.0, workspace=ws)
+        return da, db
+
+    inf = float("inf")
+    for start in (7.0, 0.5):                        # (7: overwritten)
+        for p, q in zip(grads([1.0, 2.0, 1.0, 1.0], start), grads([float("nan"), 2.0, inf, -inf], start)):
+            assert torch.equal(p, q) and (q[[0, 2, 3]] == (0.0 if start == 7.0 else start)).all() and torch.isfinite(q).all()
