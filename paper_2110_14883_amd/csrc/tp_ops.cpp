@@ -341,7 +341,7 @@ int tp_dropout_bwd(const tp_dropout_t* drop, const void* dy, int64_t ld_dy, cons
     if (!aligned16(dy) || !aligned16(dx) || (cols & 7) || (ld_dy & 7) || (ld_dx & 7)) return TP_ERR_ALIGN;
     if (preact && (!aligned16(preact) || (ld_pre & 7))) return TP_ERR_ALIGN;
     if (db_f32 && !aligned16(db_f32)) return TP_ERR_ALIGN;
-    if (ld_dy < cols || ld_dx < cols || (preact && ld_pre < cols)) return TP_ERR_SHAPE;
+    if (rows > 0 && (ld_dy < cols || ld_dx < cols || (preact && ld_pre < cols))) return TP_ERR_SHAPE;
     DropArgs a;
     if (int e = check_dropout(drop, 0, 0, rows, cols, &a)) return e;
     if (db_f32 && workspace && (!aligned16(workspace) || workspace_bytes < colsum_ws_bytes(rows, cols))) return TP_ERR_WORKSPACE;

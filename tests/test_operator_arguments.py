@@ -172,3 +172,15 @@ def test_dropout_outputs_that_overlap_what_is_read_are_refused():
     assert f((at, cols, f32), far, res=(0x900000, 72)) == 4 and f((at, cols, f32), (0x900000, cols, f32), res=(0x900000, cols)) == 4
     assert f((at, cols, f32), far, pre=far) == 4 and f((at, cols, f32), far, pre=(at, cols, bf)) == 4 and f((at, cols, f32), far, res=(0x500000, cols), pre=(0x500010, cols, bf)) == 4
     assert b((at, cols), (at + 16, cols)) == 4 and b((at, cols), (at, 72)) == 4 and b((at, cols), (0x900000, cols), pre=(0x900080, cols)) == 4
+
+
+def test_empty_dropout_calls_need_no_blocks():
+    """Nothing to do with no rows or columns, blocks left out and of any leading dimension."""
+    d = T.Dropout(0.1, 1)
+    T.tp_dropout_fwd(d, None, None, T.EPI_BIAS, None, rows=0, cols=64, stream=0)
+    T.tp_dropout_fwd(d, None, None, T.EPI_BIAS, None, rows=4, cols=0, stream=0)
+    T.tp_dropout_bwd(d, None, None, rows=0, cols=64, stream=0)
+    T.tp_dropout_bwd(d, None, None, rows=4, cols=0, stream=0)
+    T.tp_dropout_bwd(d, (0x10000, 8), (0x20000, 8), preact=(0x30000, 8), rows=0, cols=64, stream=0)
+    # what does not depend on the extents is still looked at
+    assert status(lambda: T.tp_dropout_bwd(T.Dropout(1.5, 1), None, None, rows=0, cols=64, stream=0)) == 2 and status(lambda: T.tp_dropout_bwd(d, None, None, db=0x40004, rows=0, cols=64, stream=0)) == 5

@@ -148,3 +148,9 @@ def test_scales_of_adapters_without_rows_do_not_matter(m):
     for start in (7.0, 0.5):                        # (7: overwritten)
         for p, q in zip(grads([1.0, 2.0, 1.0, 1.0], start), grads([float("nan"), 2.0, inf, -inf], start)):
             assert torch.equal(p, q) and (q[[0, 2, 3]] == (0.0 if start == 7.0 else start)).all() and torch.isfinite(q).all()
+
+
+def test_bias_gradient_of_no_rows_without_blocks():
+    db = torch.full((72,), 7.0, device="cuda")
+    T.tp_dropout_bwd(T.Dropout(0.1, 1), None, None, db=db, rows=0, cols=64)
+    assert (db[:64] == 0).all() and (db[64:] == 7).all()
