@@ -301,6 +301,7 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
 int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_dtype, const void* bias, int epi, tp_cblk_t residual, tp_oblk_t y,
                    tp_oblk_t preact, int64_t rows, int64_t cols, void* hip_stream) {
     if (!drop) return TP_ERR_NULL;
+    if (rows < 0 || cols < 0) return TP_ERR_SHAPE;
     if (rows == 0 || cols == 0) {                // (an empty tensor has no address)
         DropArgs a;
         return check_dropout(drop, 0, 0, rows, cols, &a);
@@ -309,7 +310,6 @@ int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_
     if (epi != TP_EPI_NONE && epi != TP_EPI_BIAS && epi != TP_EPI_BIAS_GELU) return TP_ERR_MODE;
     if (epi != TP_EPI_NONE && !bias) return TP_ERR_NULL;
     if (x_dtype != TP_F32 && x_dtype != TP_BF16) return TP_ERR_DTYPE;
-    if (rows < 0 || cols < 0) return TP_ERR_SHAPE;
     if (!aligned16(x) || (bias && !aligned16(bias)) || (ld_x & 7)) return TP_ERR_ALIGN;
     if (ld_x < cols) return TP_ERR_SHAPE;
     if (int e = check_oblk(y, cols, false)) return e;

@@ -184,3 +184,11 @@ def test_empty_dropout_calls_need_no_blocks():
     T.tp_dropout_bwd(d, (0x10000, 8), (0x20000, 8), preact=(0x30000, 8), rows=0, cols=64, stream=0)
     # what does not depend on the extents is still looked at
     assert status(lambda: T.tp_dropout_bwd(T.Dropout(1.5, 1), None, None, rows=0, cols=64, stream=0)) == 2 and status(lambda: T.tp_dropout_bwd(d, None, None, db=0x40004, rows=0, cols=64, stream=0)) == 5
+
+
+def test_negative_extents_of_dropout_are_refused():
+    """Also where the other one is zero."""
+    d = T.Dropout(0.1, 1)
+    for rows, cols in ((0, -8), (-1, 0), (-1, -8), (-1, 64), (4, -8)):
+        assert status(lambda: T.tp_dropout_fwd(d, (0x10000, 64, B.DT_BF16), None, T.EPI_NONE, (0x20000, 64, B.DT_BF16), rows=rows, cols=cols, stream=0)) == 4
+        assert status(lambda: T.tp_dropout_bwd(d, (0x10000, 64), (0x20000, 64), rows=rows, cols=cols, stream=0)) == 4
