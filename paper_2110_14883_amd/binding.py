@@ -74,7 +74,7 @@ class _Factor(C.Structure):
 
 class Adapters(NamedTuple):
     """Which rows use which adapter of a pool (tp_adapters_t): int32 device tensors offsets [n_segments + 1] and ids [n_segments] (an id outside the pool:
-    none), and the adapters' scales (fp32 device tensor, None: all 1).  The factors are tensors [n_adapters, rank, cols]."""
+    none), and the adapters' scales (fp32 device tensor, None: all 1).  n_segments may be left out where ids is a tensor.  The factors are tensors [n_adapters, rank, cols]."""
     offsets: Any
     ids: Any
     n_adapters: int

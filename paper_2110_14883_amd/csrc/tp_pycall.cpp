@@ -481,7 +481,7 @@ PyObject* dropout_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return f_dropout_bwd(&d, dy.ptr, dy.ld, pre.ptr, pre.ld, const_cast<void*>(dx.ptr), dx.ld, db, rows, cols, ws.ptr, ws.bytes, stream);
     });
 }
-// A call's adapters: a sequence (offsets, ids, n_adapters, rank, scale, n_segments); n_segments None: as many as ids has
+// A call's adapters: a sequence (offsets, ids, n_adapters, rank, scale, n_segments); n_segments None: as many as ids, a tensor, has
 bool to_adapters(PyObject* o, tp_adapters_t* a, Devices* at) {
     Ref s(PySequence_Fast(o, "adapters must be an Adapters"));
     if (!s) return false;
@@ -496,7 +496,13 @@ bool to_adapters(PyObject* o, tp_adapters_t* a, Devices* at) {
     if (!look(it[0], g_i32, at) || !look(it[1], g_i32, at) || !look(it[4], g_f32, at) || !to_ptr(it[0], &offsets) || !to_ptr(it[1], &ids) ||
         !to_int(it[2], &pool) || !to_int(it[3], &rank) || !to_ptr(it[4], &scale) || (it[5] != Py_None && !to_i64(it[5], &n)))
         return false;
-    if (it[5] == Py_None && it[1] != Py_None && !PyLong_Check(it[1]) && !numel(it[1], &n)) return false;
+    if (it[5] == Py_None && it[1] != Py_None) {
+        if (PyLong_Check(it[1])) {
+            PyErr_SetString(PyExc_ValueError, "n_segments is needed where ids is an address");
+            return false;
+        }
+        if (!numel(it[1], &n)) return false;
+    }
     if (n < 0 || n > INT32_MAX - 1) n = -1;                              // (the library answers)
     if (!flat(it[0], n > 0 ? n + 1 : 0, "offsets") || !flat(it[1], n > 0 ? n : 0, "ids") || !flat(it[4], pool, "scale")) return false;
     *a = tp_adapters_t{static_cast<const int32_t*>(offsets), static_cast<const int32_t*>(ids), static_cast<const float*>(scale), (int32_t)n, pool, rank};

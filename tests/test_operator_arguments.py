@@ -192,3 +192,12 @@ def test_negative_extents_of_dropout_are_refused():
     for rows, cols in ((0, -8), (-1, 0), (-1, -8), (-1, 64), (4, -8)):
         assert status(lambda: T.tp_dropout_fwd(d, (0x10000, 64, B.DT_BF16), None, T.EPI_NONE, (0x20000, 64, B.DT_BF16), rows=rows, cols=cols, stream=0)) == 4
         assert status(lambda: T.tp_dropout_bwd(d, (0x10000, 64), (0x20000, 64), rows=rows, cols=cols, stream=0)) == 4
+
+
+def test_adapters_by_address_need_their_number_of_segments(device0):
+    """There is no tensor to count them by: an error instead of a call that does nothing.  With none at all there is nothing to count."""
+    for ad in (T.Adapters(0x100, 0x200, 2, RANK), T.Adapters(Block(4, dtype=I32), 0x200, 2, RANK)):
+        with pytest.raises(ValueError, match="n_segments"):
+            fwd(ad=ad)
+    assert status(lambda: fwd(ad=T.Adapters(0x100, 0x200, 2, RANK, None, 3))) == 7 and status(lambda: fwd(ad=AD._replace(n_segments=2))) == 7
+    assert status(lambda: fwd(ad=T.Adapters(None, None, 2, RANK))) == 7
