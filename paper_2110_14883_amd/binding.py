@@ -216,9 +216,9 @@ def _call():
     spec.loader.exec_module(m)
     try:
         import torch
-        dtypes, more, device = (torch.float32, torch.bfloat16), (torch.int32, torch.Tensor), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        dtypes, more, device = (torch.float32, torch.bfloat16), (torch.int32, torch.int64, getattr(torch, "uint64", None), torch.Tensor), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     except ImportError:                      # blocks are then (address, leading dimension[, dtype]) sequences
-        dtypes, more, device = (None, None), (None, None), None
+        dtypes, more, device = (None, None), (None,) * 4, None
     names = ("tp_linear_fwd_ex", "tp_linear_fwd_static", "tp_linear_bwd_ex", "tp_linear_bwd_partials_ex", "tp_bias_act", "tp_dgelu",
              "tp_bias_grad")
     m.bind(*[C.cast(getattr(L, n), C.c_void_p).value for n in names], *dtypes)

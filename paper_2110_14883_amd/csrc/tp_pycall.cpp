@@ -19,7 +19,7 @@ namespace {
 PyObject *s_data_ptr, *s_stride, *s_shape, *s_dtype, *s_numel, *s_element_size;      // interned names
 PyObject *s_get_device, *s_is_contiguous;
 PyObject* g_tensor;                                                                  // torch.Tensor, or None
-PyObject *g_i32, *g_f32, *g_bf16;                                                            // torch.int32, torch.float32, torch.bfloat16
+PyObject *g_i32, *g_i64, *g_u64, *g_f32, *g_bf16;                                    // torch.int32, torch.int64, torch.uint64, torch.float32, torch.bfloat16
 PyObject *g_current_device;                                                          // callable, or None: its answer is not compared
 
 decltype(&tp_block_map) f_block_map;
@@ -452,9 +452,10 @@ bool to_dropout(PyObject* o, tp_dropout_t* d, Devices* at) {
         return false;
     if (it[3] != Py_None && !PyLong_Check(it[3])) {
         bool tensor;
-        int64_t size = 8;
-        if (!is_tensor(it[3], &tensor) || (tensor && !call0(it[3], s_element_size, &size))) return false;
-        if (size != 8) { PyErr_SetString(PyExc_TypeError, "offset_dev must be a 64-bit integer"); return false; }
+        if (!is_tensor(it[3], &tensor)) return false;
+        Ref dt(tensor ? PyObject_GetAttr(it[3], s_dtype) : nullptr);
+        if (tensor && !dt) return false;
+        if (tensor && dt.p != g_i64 && dt.p != g_u64) { PyErr_SetString(PyExc_TypeError, "offset_dev must be a 64-bit integer"); return false; }
     }
     d->seed = (uint64_t)seed;
     d->offset = (uint64_t)offset;
@@ -638,15 +639,17 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-// bind_ops(addresses of the functions behind those and of tp_block_map, torch.int32, torch.Tensor, a function that gives the current device or None)
+// bind_ops(addresses of the functions behind those and of tp_block_map, torch.int32, torch.int64, torch.uint64, torch.Tensor, a function that gives the current device or None)
 PyObject* bind_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* f[5];
-    if (!count(n, 8)) return nullptr;
+    if (!count(n, 10)) return nullptr;
     for (int i = 0; i < 5; ++i)
         if (!to_ptr(a[i], &f[i])) return nullptr;
     Py_INCREF(a[5]); Py_XSETREF(g_i32, a[5]);
-    Py_INCREF(a[6]); Py_XSETREF(g_tensor, a[6]);
-    Py_INCREF(a[7]); Py_XSETREF(g_current_device, a[7]);
+    Py_INCREF(a[6]); Py_XSETREF(g_i64, a[6]);
+    Py_INCREF(a[7]); Py_XSETREF(g_u64, a[7]);
+    Py_INCREF(a[8]); Py_XSETREF(g_tensor, a[8]);
+    Py_INCREF(a[9]); Py_XSETREF(g_current_device, a[9]);
     f_block_map = reinterpret_cast<decltype(f_block_map)>(f[4]);
     f_adapter_fwd = reinterpret_cast<decltype(f_adapter_fwd)>(f[2]);
     f_adapter_bwd = reinterpret_cast<decltype(f_adapter_bwd)>(f[3]);

@@ -201,3 +201,13 @@ def test_adapters_by_address_need_their_number_of_segments(device0):
             fwd(ad=ad)
     assert status(lambda: fwd(ad=T.Adapters(0x100, 0x200, 2, RANK, None, 3))) == 7 and status(lambda: fwd(ad=AD._replace(n_segments=2))) == 7
     assert status(lambda: fwd(ad=T.Adapters(None, None, 2, RANK))) == 7
+
+
+def test_the_offset_on_the_device_is_a_64_bit_integer(device0):
+    """Other types of eight bytes would be read as integers."""
+    for dtype in (torch.float64, torch.complex64, torch.int32, torch.float32):
+        with pytest.raises(TypeError):
+            T.tp_dropout_bwd(T.Dropout(2.0, 1, 0, Block(1, dtype=dtype)), Block(M, F), Block(M, F, at=0x200000), stream=0)
+    for dtype in (torch.int64, torch.uint64):
+        assert status(lambda: T.tp_dropout_bwd(T.Dropout(2.0, 1, 0, Block(1, dtype=dtype)), Block(M, F), Block(M, F, at=0x200000), stream=0)) == 2
+    assert status(lambda: T.tp_dropout_bwd(T.Dropout(2.0, 1, 0, 0x1000), Block(M, F), Block(M, F, at=0x200000), stream=0)) == 2
