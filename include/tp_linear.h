@@ -412,8 +412,9 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
                    tp_factor_out_t da, const tp_cblk_t* dy_own, const float* v, tp_factor_out_t db, int accumulate, void* workspace,
                    size_t workspace_bytes, void* hip_stream);
 
-/* Bytes of device workspace tp_adapter_fwd (TP_PASS_FWD) or tp_adapter_bwd (TP_PASS_DX) may need: planes of V or U, and of dA and dB where their rows
- * are shared out.  Only n_segments, n_adapters and rank of `adapters` are looked at.  0 on invalid arguments.  Host only. */
+/* Bytes of device workspace tp_adapter_fwd (TP_PASS_FWD) or tp_adapter_bwd (TP_PASS_DX) may need with n_segments or any smaller number of them: planes of
+ * V or U, and of dA and dB where their rows are shared out (up to 32 of each adapter in the pool).  Only n_segments, n_adapters and rank of `adapters`
+ * are looked at.  0 on invalid arguments.  Host only. */
 size_t tp_adapter_workspace_size(const tp_grid_t* grid, const tp_dims_t* dims, int pass, const tp_adapters_t* adapters);
 
 /* Human-readable name of a status code (static storage). */

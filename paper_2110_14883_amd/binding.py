@@ -379,6 +379,7 @@ def tp_dropout_bwd(dropout: Dropout, dy, dx, preact=None, db=None, rows: int | N
 
 
 def tp_adapter_workspace_size(grid: Grid, dims, pass_: int, adapters: Adapters) -> int:
+    """Bytes for these adapters' number of segments and any smaller one."""
     n = adapters.n_segments if adapters.n_segments is not None else adapters.ids.numel()
     g, d, a = grid._c(), _dims(dims), _AdaptersS(None, None, None, int(n), int(adapters.n_adapters), int(adapters.rank))
     return int(lib().tp_adapter_workspace_size(C.byref(g), C.byref(d), int(pass_), C.byref(a)))

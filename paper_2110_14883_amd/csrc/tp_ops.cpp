@@ -73,7 +73,7 @@ int check_over(const tp_oblk_t& c, const tp_oblk_t& y, int64_t rows, int64_t col
 
 // Tiles of at most `tile` rows that segments over `rows` rows can have
 int64_t most_tiles(int64_t rows, int64_t segments, int tile) {
-    const int64_t some = std::min(rows, segments);        // segments with rows
+    const int64_t some = std::min(rows, std::max<int64_t>(1, segments));        // segments with rows (none: as one)
     return (rows + some * (tile - 1)) / tile;
 }
 // How the products run.
@@ -132,22 +132,28 @@ bool in_one_launch(const Split& s, int64_t rows, int64_t segments, int64_t facto
 // rows, two of 12 adapters, 32 ranks 83.4 -> 67.9; 8124 rows in two segments, 27 adapters, 16 ranks 25.7 -> 22; without the average: 642 rows in 28
 // segments, ten adapters, 64 ranks 35 -> 21.
 int64_t grad_blocks(int64_t cols, int pool, int rank) { return (cols + 127) / 128 * ((rank + 31) / 32) * pool; }
+int64_t grad_busy(int64_t segments, int pool) { return std::max<int64_t>(1, std::min<int64_t>(pool, segments)); }     // adapters that can have rows
+int64_t grad_enough(int64_t cols, int rank, int64_t adapters) { const int64_t blocks = grad_blocks(cols, 1, rank) * adapters; return (512 + blocks - 1) / blocks; }
+int64_t grad_room(int64_t cols, int pool, int rank) { return std::max<int64_t>(grad_enough(cols, rank, pool), 256 / pool); }
 int plan_grad(int64_t rows, int64_t segments, int64_t cols, int pool, int rank) {
-    auto enough = [&](int64_t adapters) { const int64_t blocks = grad_blocks(cols, 1, rank) * adapters; return (512 + blocks - 1) / blocks; };
-    const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(pool, segments)), most = std::max<int64_t>(enough(pool), 256 / pool), units = most_tiles(rows, segments, 32);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({enough(busy), most, units / 4, std::max<int64_t>(1, units / (2 * busy)), 32}));
+    const int64_t busy = grad_busy(segments, pool), units = most_tiles(rows, segments, 32);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({grad_enough(cols, rank, busy), grad_room(cols, pool, rank), units / 4, std::max<int64_t>(1, units / (2 * busy)), 32}));
+}
+// The most of these that any number of segments up to this one takes: a program has one workspace for batches of more and fewer requests.  K is shared most with
+// one segment, which has the fewest tiles (64 rows make more than 128 of them where they are chosen, and K is not shared then); of the shares every bound where it is largest.
+int most_splits(int64_t rows, int64_t k, int n_steps, int64_t up_cols, int rank, bool bwd) { return plan_products(rows, 1, k, n_steps, up_cols, rank, bwd).splits; }
+int most_shares(int64_t rows, int64_t segments, int64_t cols, int pool, int rank) {
+    const int64_t units = most_tiles(rows, segments, 32), busy = segments > pool ? pool : 1;
+    const int64_t average = std::max(most_tiles(rows, 1, 32) / 2, (segments > pool ? units : 0) / (2 * busy));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({grad_enough(cols, rank, 1), grad_room(cols, pool, rank), units / 4, std::max<int64_t>(1, average), 32}));
 }
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 // the workspace, in this order
 struct Space { size_t low, da, db, units; size_t all() const { return padded(low) + padded(da) + padded(db) + padded(units); } };
-Space space_fwd(const Map& f, const tp_adapters_t* a) {
-    const Split s = plan_products(f.m, a->n_segments, f.k, f.n_steps, f.n, a->rank, false);
-    return Space{(size_t)s.splits * (size_t)f.m * a->rank * 4, 0, 0, 0};
-}
-Space space_bwd(const Map& f, const Map& x, const tp_adapters_t* a) {
-    const Split s = plan_products(x.m, a->n_segments, x.k, x.n_steps, x.n, a->rank, true);
-    const size_t shares = (size_t)plan_grad(x.m, a->n_segments, x.n + f.n, a->n_adapters, a->rank), each = shares * a->n_adapters * a->rank * 4;
-    Space w{(size_t)s.splits * (size_t)x.m * a->rank * 4, 0, 0, 0};
+Space space_fwd(const Map& f, const tp_adapters_t* a, int splits) { return Space{(size_t)splits * (size_t)f.m * a->rank * 4, 0, 0, 0}; }
+Space space_bwd(const Map& f, const Map& x, const tp_adapters_t* a, int splits, int shares) {
+    const size_t each = (size_t)shares * a->n_adapters * a->rank * 4;
+    Space w{(size_t)splits * (size_t)x.m * a->rank * 4, 0, 0, 0};
     if (shares > 1) { w.da = each * x.n; w.db = each * f.n; w.units = (size_t)a->n_adapters * 4; }
     return w;
 }
@@ -190,7 +196,10 @@ extern "C" {
 size_t tp_adapter_workspace_size(const tp_grid_t* grid, const tp_dims_t* dims, int pass, const tp_adapters_t* adapters) {
     Map f, x;
     if (check_counts(adapters) != TP_OK || block_map(grid, dims, TP_PASS_FWD, &f) != TP_OK || block_map(grid, dims, TP_PASS_DX, &x) != TP_OK) return 0;
-    return pass == TP_PASS_FWD ? space_fwd(f, adapters).all() : pass == TP_PASS_DX ? space_bwd(f, x, adapters).all() : 0;
+    if (pass == TP_PASS_FWD) return space_fwd(f, adapters, most_splits(f.m, f.k, f.n_steps, f.n, adapters->rank, false)).all();
+    if (pass != TP_PASS_DX) return 0;
+    const int shares = most_shares(x.m, std::max(1, adapters->n_segments), x.n + f.n, adapters->n_adapters, adapters->rank);
+    return space_bwd(f, x, adapters, most_splits(x.m, x.k, x.n_steps, x.n, adapters->rank, true), shares).all();
 }
 
 int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, const tp_adapters_t* adapters, const tp_cblk_t* x_blocks,
@@ -210,7 +219,7 @@ int tp_adapter_fwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
     }
     const Split sp = plan_products(s.m, adapters->n_segments, s.k, s.n_steps, s.n, adapters->rank, false);
     if (int e = check_tiles(sp)) return e;
-    const Space need = space_fwd(s, adapters);
+    const Space need = space_fwd(s, adapters, sp.splits);
     float* const planes = v && sp.splits == 1 ? v : static_cast<float*>(workspace);
     DownArgs d{};
     if (int e = fill_down(d, sp, adapters, n_steps, x_blocks, a_blocks, s.m, s.k, planes)) return e;
@@ -255,7 +264,8 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
     const Split sp = plan_products(x.m, adapters->n_segments, x.k, x.n_steps, x.n, adapters->rank, true);
     if (int e = check_tiles(sp)) return e;
     if (grad_blocks(x.n + f.n, adapters->n_adapters, adapters->rank) > kMostGradBlocks) return TP_ERR_SHAPE;
-    const Space need = space_bwd(f, x, adapters);
+    const int shares = plan_grad(x.m, adapters->n_segments, x.n + f.n, adapters->n_adapters, adapters->rank);
+    const Space need = space_bwd(f, x, adapters, sp.splits, shares);
     char* at = static_cast<char*>(workspace);
     float* const planes = reinterpret_cast<float*>(at);
     DropArgs mask{};
@@ -285,7 +295,7 @@ int tp_adapter_bwd(const tp_grid_t* grid, const tp_dims_t* dims, int n_steps, co
         if (int e = side(planes, sp.splits, *x_own, x.n, drop != nullptr, da, padded(need.low))) return e;
     if (db.ptr)
         if (int e = side(v, 1, *dy_own, f.n, 0, db, padded(need.low) + padded(need.da))) return e;
-    g.rank = adapters->rank; g.shares = plan_grad(x.m, adapters->n_segments, x.n + f.n, adapters->n_adapters, adapters->rank); g.accumulate = accumulate != 0;
+    g.rank = adapters->rank; g.shares = shares; g.accumulate = accumulate != 0;
     g.scale = adapters->scale; g.seg = segments(adapters, x.m); g.drop = mask;
     g.units = reinterpret_cast<int32_t*>(at + padded(need.low) + padded(need.da) + padded(need.db));
     if (!want_u && !db.ptr) return TP_OK;

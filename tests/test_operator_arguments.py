@@ -211,3 +211,13 @@ def test_the_offset_on_the_device_is_a_64_bit_integer(device0):
     for dtype in (torch.int64, torch.uint64):
         assert status(lambda: T.tp_dropout_bwd(T.Dropout(2.0, 1, 0, Block(1, dtype=dtype)), Block(M, F), Block(M, F, at=0x200000), stream=0)) == 2
     assert status(lambda: T.tp_dropout_bwd(T.Dropout(2.0, 1, 0, 0x1000), Block(M, F), Block(M, F, at=0x200000), stream=0)) == 2
+
+
+@pytest.mark.parametrize("m,h,f", [(1, 64, 64), (20, 4096, 512), (33, 16384, 128), (200, 4096, 4096), (700, 1504, 2496), (8200, 4096, 4096), (40000, 1280, 5120)])
+def test_a_workspace_serves_every_smaller_number_of_segments(m, h, f):
+    """The size for n segments is never below that for fewer, so one made for the most requests there can be is enough for any."""
+    for pool in (1, 3, 8, 40, 300):
+        for rank in (8, 16, 64, 128):
+            for which in (T.PASS_FWD, T.PASS_DX):
+                sizes = [T.tp_adapter_workspace_size(GRID, (m, h, f), which, T.Adapters(None, None, pool, rank, None, n)) for n in (*range(0, 60), 97, 300, 301, 1000, 9000, 50000)]
+                assert sizes == sorted(sizes) and sizes[0] > 0, (pool, rank, which)

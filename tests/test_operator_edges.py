@@ -154,3 +154,28 @@ def test_bias_gradient_of_no_rows_without_blocks():
     db = torch.full((72,), 7.0, device="cuda")
     T.tp_dropout_bwd(T.Dropout(0.1, 1), None, None, db=db, rows=0, cols=64)
     assert (db[:64] == 0).all() and (db[64:] == 7).all()
+
+
+@pytest.mark.parametrize("m,pool,rank", [(200, 8, 16), (2050, 3, 16), (3000, 8, 64)])
+def test_one_workspace_for_every_number_of_segments(m, pool, rank):
+    """A workspace made for the largest number of requests serves calls of fewer, forward and backward, and they give what they give with their own."""
+    h, n, most = 1024, 136, 12
+    g = _g(80)
+    grid, dims = T.Grid(T.MODE_1D_COL), (m, h, n)
+    x, a, b, c, dy = _strided(g, m, h), _strided(g, pool, rank, h), _strided(g, pool, rank, n), _strided(g, m, n), _strided(g, m, n)
+    size = lambda count: max(T.tp_adapter_workspace_size(grid, dims, q, T.Adapters(None, None, pool, rank, None, count)) for q in (T.PASS_FWD, T.PASS_DX))
+    room = torch.full((size(most) + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+
+    def both(count, ws):
+        cuts = [i * m // count for i in range(count + 1)]
+        ad = T.Adapters(i32(cuts), i32([i % pool for i in range(count)]), pool, rank)
+        y, v, dx = torch.empty(m, n, dtype=BF, device="cuda"), torch.empty(m, rank, device="cuda"), torch.empty(m, h, device="cuda")
+        da, db = torch.empty(pool, rank, h, device="cuda"), torch.empty(pool, rank, n, device="cuda")
+        T.tp_adapter_fwd(grid, dims, 1, ad, [x], [a], b, c, None, 0, y, v=v, workspace=ws)
+        T.tp_adapter_bwd(grid, dims, 1, ad, [dy], [b], a=a, dx_base=x, dx=dx, x_own=x, da=da, dy_own=dy, v=v, db=db, workspace=ws)
+        return y, v, dx, da, db
+
+    for count in (1, 2, 3, 5, 9, most):
+        for p, q in zip(both(count, room[:-64]), both(count, torch.empty(size(count), dtype=torch.uint8, device="cuda"))):
+            assert torch.equal(p, q), count
+    assert (room[-64:] == 0xFF).all()
