@@ -320,7 +320,7 @@ size_t tp_bias_grad_workspace_size(int64_t rows, int64_t cols);
  *   row0, col0   : where the block's first element lies in the full matrix; col0 a multiple of 8.
  *   p            : probability of dropping, 0 <= p <= 1 (p = 1 drops everything).
  * Refused: p outside [0, 1] or NaN (TP_ERR_MODE), col0 not a multiple of 8 or offset_dev misaligned (TP_ERR_ALIGN), negative positions, rows that
- * end beyond 2^32 or columns beyond 2^35 (TP_ERR_SHAPE).
+ * end beyond 2^32 or columns beyond 2^35, and blocks of 2^32 columns or more (TP_ERR_SHAPE).
  */
 typedef struct { uint64_t seed, offset; const uint64_t* offset_dev; int64_t row0, col0; double p; } tp_dropout_t;
 

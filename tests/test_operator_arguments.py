@@ -221,3 +221,13 @@ def test_a_workspace_serves_every_smaller_number_of_segments(m, h, f):
             for which in (T.PASS_FWD, T.PASS_DX):
                 sizes = [T.tp_adapter_workspace_size(GRID, (m, h, f), which, T.Adapters(None, None, pool, rank, None, n)) for n in (*range(0, 60), 97, 300, 301, 1000, 9000, 50000)]
                 assert sizes == sorted(sizes) and sizes[0] > 0, (pool, rank, which)
+
+
+def test_dropout_rows_longer_than_the_kernels_count():
+    """Columns are numbered in 32 bits inside a block, whatever its place in the full matrix."""
+    d, n = T.Dropout(0.1, 1), 1 << 32
+    assert status(lambda: T.tp_dropout_fwd(d, (1 << 40, n, B.DT_BF16), None, T.EPI_NONE, (1 << 45, n, B.DT_BF16), rows=1, cols=n, stream=0)) == 4
+    assert status(lambda: T.tp_dropout_bwd(d, (1 << 40, n), (1 << 45, n), rows=1, cols=n, stream=0)) == 4
+    for n in ((1 << 32) - 8, 64):           # (the probability is what is refused there)
+        assert status(lambda: T.tp_dropout_fwd(T.Dropout(2.0, 1, col0=1 << 34), (1 << 40, n, B.DT_BF16), None, T.EPI_NONE, (1 << 45, n, B.DT_BF16), rows=1, cols=n, stream=0)) == 2
+        assert status(lambda: T.tp_dropout_bwd(T.Dropout(2.0, 1, col0=1 << 34), (1 << 40, n), (1 << 45, n), rows=1, cols=n, stream=0)) == 2
