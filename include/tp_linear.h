@@ -340,7 +340,7 @@ int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_
 
 /*
  * tp_dropout_bwd -- its gradient:  dx = drop'(dy) GeLU'(preact)  (without preact: drop'(dy)), bf16, and optionally db (fp32 [cols]): the
- * column sums of dx before its rounding, in an order fixed by (rows, cols) and whether there is a workspace.  The residual's gradient is dy itself.
+ * column sums of dx before its rounding, in an order fixed by (rows, cols) and whether there is a workspace (up to 2^30 - 256 columns then, else TP_ERR_SHAPE).  The residual's gradient is dy itself.
  *   drop      : as in forward.   dy, preact, dx: bf16 [rows, cols];  dx may be dy or preact itself (same leading dimension), else must not overlap it (TP_ERR_SHAPE).
  *   workspace : as in tp_bias_grad (tp_bias_grad_workspace_size(rows, cols) bytes, 16-byte aligned, or NULL); read only if db is wanted.
  * With rows = 0 db is all zeros (blocks may be NULL then).  Errors: as tp_dropout_fwd, and TP_ERR_WORKSPACE.

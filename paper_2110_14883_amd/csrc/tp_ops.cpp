@@ -13,6 +13,7 @@ using namespace tpl;
 namespace {
 
 constexpr int64_t kMostCols = ((int64_t)1 << 32) - 8;     // of a block of the dropout calls: its columns are numbered in 32 bits
+constexpr int64_t kMostSumCols = ((int64_t)1 << 30) - 256;  // with their sums, strips of 64 or 256 columns at four threads a column: fewer than 2^32 threads
 
 // A mask whose block begins at (row, col) behind the caller's own position
 int check_dropout(const tp_dropout_t* d, int64_t row, int64_t col, int64_t rows, int64_t cols, DropArgs* a) {
@@ -349,7 +350,7 @@ int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_
 int tp_dropout_bwd(const tp_dropout_t* drop, const void* dy, int64_t ld_dy, const void* preact, int64_t ld_pre, void* dx, int64_t ld_dx, void* db_f32,
                    int64_t rows, int64_t cols, void* workspace, size_t workspace_bytes, void* hip_stream) {
     if (!drop || (rows != 0 && cols != 0 && (!dy || !dx))) return TP_ERR_NULL;
-    if (rows < 0 || cols < 0 || cols > kMostCols || (db_f32 && cols > INT32_MAX)) return TP_ERR_SHAPE;
+    if (rows < 0 || cols < 0 || cols > kMostCols || (db_f32 && cols > kMostSumCols)) return TP_ERR_SHAPE;
     if (!aligned16(dy) || !aligned16(dx) || (cols & 7) || (ld_dy & 7) || (ld_dx & 7)) return TP_ERR_ALIGN;
     if (preact && (!aligned16(preact) || (ld_pre & 7))) return TP_ERR_ALIGN;
     if (db_f32 && !aligned16(db_f32)) return TP_ERR_ALIGN;

@@ -231,3 +231,10 @@ def test_dropout_rows_longer_than_the_kernels_count():
     for n in ((1 << 32) - 8, 64):           # (the probability is what is refused there)
         assert status(lambda: T.tp_dropout_fwd(T.Dropout(2.0, 1, col0=1 << 34), (1 << 40, n, B.DT_BF16), None, T.EPI_NONE, (1 << 45, n, B.DT_BF16), rows=1, cols=n, stream=0)) == 2
         assert status(lambda: T.tp_dropout_bwd(T.Dropout(2.0, 1, col0=1 << 34), (1 << 40, n), (1 << 45, n), rows=1, cols=n, stream=0)) == 2
+
+
+def test_bias_gradients_of_more_columns_than_a_launch_has_threads_for():
+    """Four threads a column, 2^32 - 1 in a launch: refused before it."""
+    d, call = T.Dropout(0.1, 1), lambda d, n: status(lambda: T.tp_dropout_bwd(d, (1 << 40, n), (1 << 45, n), db=1 << 48, rows=1, cols=n, stream=0))
+    assert call(d, 1 << 30) == 4 and call(d, (1 << 30) - 248) == 4 and call(d, (1 << 31) - 8) == 4
+    assert call(T.Dropout(2.0, 1), (1 << 30) - 256) == 2
