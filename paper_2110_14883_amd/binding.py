@@ -205,6 +205,11 @@ def lib() -> C.CDLL:
     return _lib
 
 
+def _hip_get_device(L) -> int:
+    """Address of hipGetDevice in the runtime that the library launches with."""
+    return C.cast(L.hipGetDevice, C.c_void_p).value
+
+
 @functools.lru_cache(maxsize=1)
 def _call():
     """The extension module that makes the calls, given the loaded library's functions."""
@@ -216,14 +221,14 @@ def _call():
     spec.loader.exec_module(m)
     try:
         import torch
-        dtypes, more, device = (torch.float32, torch.bfloat16), (torch.int32, torch.int64, getattr(torch, "uint64", None), torch.Tensor), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        dtypes, more = (torch.float32, torch.bfloat16), (torch.int32, torch.int64, getattr(torch, "uint64", None), torch.Tensor)
     except ImportError:                      # blocks are then (address, leading dimension[, dtype]) sequences
-        dtypes, more, device = (None, None), (None,) * 4, None
+        dtypes, more = (None, None), (None,) * 4
     names = ("tp_linear_fwd_ex", "tp_linear_fwd_static", "tp_linear_bwd_ex", "tp_linear_bwd_partials_ex", "tp_bias_act", "tp_dgelu",
              "tp_bias_grad")
     m.bind(*[C.cast(getattr(L, n), C.c_void_p).value for n in names], *dtypes)
     ops = ("tp_dropout_fwd", "tp_dropout_bwd", "tp_adapter_fwd", "tp_adapter_bwd", "tp_block_map")
-    m.bind_ops(*[C.cast(getattr(L, n), C.c_void_p).value for n in ops], *more, device)
+    m.bind_ops(*[C.cast(getattr(L, n), C.c_void_p).value for n in ops], *more, _hip_get_device(L))
     return m
 
 
@@ -241,7 +246,10 @@ def _dims(dims) -> _DimsS:
 
 
 def _rows_cols(t, rows, cols):
-    return (t.shape[0], t.shape[1]) if rows is None else (rows, cols)
+    if rows is None:
+        s = t.shape                          # (asked for once: a tuple is made every time)
+        return s[0], s[1]
+    return rows, cols
 
 
 @functools.lru_cache(maxsize=1)

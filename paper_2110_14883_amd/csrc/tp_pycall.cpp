@@ -20,7 +20,7 @@ PyObject *s_data_ptr, *s_stride, *s_shape, *s_dtype, *s_numel, *s_element_size; 
 PyObject *s_get_device, *s_is_contiguous;
 PyObject* g_tensor;                                                                  // torch.Tensor, or None
 PyObject *g_i32, *g_i64, *g_u64, *g_f32, *g_bf16;                                    // torch.int32, torch.int64, torch.uint64, torch.float32, torch.bfloat16
-PyObject *g_current_device;                                                          // callable, or None: its answer is not compared
+int (*g_current_device)(int*);                                                       // hipGetDevice, or null: its answer is not compared
 
 decltype(&tp_block_map) f_block_map;
 decltype(&tp_linear_fwd_ex) f_fwd;
@@ -309,11 +309,8 @@ struct Devices {
             if (d == seen) return true;
         } else {
             seen = d;
-            if (!g_current_device || g_current_device == Py_None) return true;
-            Ref r(PyObject_CallNoArgs(g_current_device));
-            int64_t now;
-            if (!r || !to_i64(r.p, &now)) return false;
-            if (d == now) return true;
+            int now;
+            if (!g_current_device || (g_current_device(&now) == 0 && d == now)) return true;
         }
         PyErr_SetString(PyExc_ValueError, "the call's tensors are not all on the current device");
         return false;
@@ -335,14 +332,13 @@ bool look(PyObject* o, PyObject* want, Devices* at) {
 }
 
 bool numel(PyObject* o, int64_t* n) { return call0(o, s_numel, n); }
-// a tensor (others are taken as they are) has at least `want` elements, one behind the other
-bool flat(PyObject* t, int64_t want, const char* what) {
+// a tensor (others are taken as they are) has at least `want` elements (`have` if that is known), one behind the other
+bool flat(PyObject* t, int64_t want, const char* what, int64_t have = -1) {
     bool tensor;
     if (t == Py_None || PyLong_Check(t)) return true;
     if (!is_tensor(t, &tensor)) return false;
     if (!tensor) return true;
-    int64_t have;
-    if (!numel(t, &have)) return false;
+    if (have < 0 && !numel(t, &have)) return false;
     Ref c(PyObject_CallMethodNoArgs(t, s_is_contiguous));
     if (!c) return false;
     if (have >= want && c.p == Py_True) return true;
@@ -360,6 +356,8 @@ bool holds(const Extents& e, int64_t rows, int64_t cols) {
                  (long long)rows, (long long)cols);
     return false;
 }
+// element i of a tensor's shape or strides (tuples, of a type of their own)
+bool extent(PyObject* o, Py_ssize_t i, int64_t* out) { return PyTuple_Check(o) && i < PyTuple_GET_SIZE(o) ? to_i64(PyTuple_GET_ITEM(o, i), out) : item(o, i, out); }
 // the leading dimension of a tensor as tensor_ld() takes it, with these extents
 bool tensor_ld(PyObject* t, const Extents& e, int64_t* ld) {
     Ref st(PyObject_CallMethodNoArgs(t, s_stride)), sh(PyObject_GetAttr(t, s_shape));
@@ -368,10 +366,10 @@ bool tensor_ld(PyObject* t, const Extents& e, int64_t* ld) {
     if (n < 0) return false;
     int64_t rows = 1, cols, unit;
     if (n == 2) {
-        if (!item(sh.p, 0, &rows) || !item(sh.p, 1, &cols) || !item(st.p, 0, ld) || !item(st.p, 1, &unit)) return false;
+        if (!extent(sh.p, 0, &rows) || !extent(sh.p, 1, &cols) || !extent(st.p, 0, ld) || !extent(st.p, 1, &unit)) return false;
         if (unit == 1 || cols <= 1) return holds(e, rows, cols);
     } else if (n == 1) {
-        if (!item(sh.p, 0, &cols) || !item(st.p, 0, &unit)) return false;
+        if (!extent(sh.p, 0, &cols) || !extent(st.p, 0, &unit)) return false;
         *ld = cols;
         if (unit == 1 || cols <= 1) return holds(e, rows, cols);
     }
@@ -493,7 +491,7 @@ bool to_adapters(PyObject* o, tp_adapters_t* a, Devices* at) {
     PyObject** it = PySequence_Fast_ITEMS(s.p);
     void *offsets, *ids, *scale;
     int pool, rank;
-    int64_t n = 0;
+    int64_t n = 0, counted = -1;
     if (!look(it[0], g_i32, at) || !look(it[1], g_i32, at) || !look(it[4], g_f32, at) || !to_ptr(it[0], &offsets) || !to_ptr(it[1], &ids) ||
         !to_int(it[2], &pool) || !to_int(it[3], &rank) || !to_ptr(it[4], &scale) || (it[5] != Py_None && !to_i64(it[5], &n)))
         return false;
@@ -503,9 +501,10 @@ bool to_adapters(PyObject* o, tp_adapters_t* a, Devices* at) {
             return false;
         }
         if (!numel(it[1], &n)) return false;
+        counted = n;
     }
     if (n < 0 || n > INT32_MAX - 1) n = -1;                              // (the library answers)
-    if (!flat(it[0], n > 0 ? n + 1 : 0, "offsets") || !flat(it[1], n > 0 ? n : 0, "ids") || !flat(it[4], pool, "scale")) return false;
+    if (!flat(it[0], n > 0 ? n + 1 : 0, "offsets") || !flat(it[1], n > 0 ? n : 0, "ids", counted) || !flat(it[4], pool, "scale")) return false;
     *a = tp_adapters_t{static_cast<const int32_t*>(offsets), static_cast<const int32_t*>(ids), static_cast<const float*>(scale), (int32_t)n, pool, rank};
     return true;
 }
@@ -522,8 +521,8 @@ template <class F> bool to_factor(PyObject* o, F* f, const tp_adapters_t& a, PyO
             Ref st(PyObject_CallMethodNoArgs(o, s_stride)), sh(PyObject_GetAttr(o, s_shape));
             if (!st || !sh) return false;
             int64_t n, r, have, unit;
-            if (PySequence_Size(st.p) != 3 || !item(sh.p, 0, &n) || !item(sh.p, 1, &r) || !item(sh.p, 2, &have) ||
-                !item(st.p, 0, &stride) || !item(st.p, 1, &ld) || !item(st.p, 2, &unit)) {
+            if (PySequence_Size(st.p) != 3 || !extent(sh.p, 0, &n) || !extent(sh.p, 1, &r) || !extent(sh.p, 2, &have) ||
+                !extent(st.p, 0, &stride) || !extent(st.p, 1, &ld) || !extent(st.p, 2, &unit)) {
                 if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a factor must be [n_adapters, rank, cols]");
                 return false;
             }
@@ -639,17 +638,18 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
-// bind_ops(addresses of the functions behind those and of tp_block_map, torch.int32, torch.int64, torch.uint64, torch.Tensor, a function that gives the current device or None)
+// bind_ops(addresses of the functions behind those and of tp_block_map, torch.int32, torch.int64, torch.uint64, torch.Tensor, the address of hipGetDevice or None)
 PyObject* bind_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    void* f[5];
+    void *f[5], *get_device;
     if (!count(n, 10)) return nullptr;
     for (int i = 0; i < 5; ++i)
         if (!to_ptr(a[i], &f[i])) return nullptr;
+    if (!to_ptr(a[9], &get_device)) return nullptr;
     Py_INCREF(a[5]); Py_XSETREF(g_i32, a[5]);
     Py_INCREF(a[6]); Py_XSETREF(g_i64, a[6]);
     Py_INCREF(a[7]); Py_XSETREF(g_u64, a[7]);
     Py_INCREF(a[8]); Py_XSETREF(g_tensor, a[8]);
-    Py_INCREF(a[9]); Py_XSETREF(g_current_device, a[9]);
+    g_current_device = reinterpret_cast<decltype(g_current_device)>(get_device);
     f_block_map = reinterpret_cast<decltype(f_block_map)>(f[4]);
     f_adapter_fwd = reinterpret_cast<decltype(f_adapter_fwd)>(f[2]);
     f_adapter_bwd = reinterpret_cast<decltype(f_adapter_bwd)>(f[3]);

@@ -1,5 +1,7 @@
 """What the calls of dropout and adapters refuse of their tensors, and what they take, seen on the host: stand-ins for tensors on the device whose addresses are
 never followed (every call that gets past the arguments is turned down by the library for its workspace or probability)."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -40,7 +42,8 @@ class Block:
 @pytest.fixture
 def device0(monkeypatch):
     """The binding with device 0 as the current one."""
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    get = C.CFUNCTYPE(C.c_int, C.POINTER(C.c_int))(lambda to: to.__setitem__(0, 0) or 0)
+    monkeypatch.setattr(B, "_hip_get_device", lambda L: C.cast(get, C.c_void_p).value)
     B._call.cache_clear()
     B._call()
     yield
