@@ -36,7 +36,9 @@ struct Bytes { const void* p; int64_t pitch, width; };
 Bytes bytes_of(const void* p, int64_t ld, int64_t cols, int dtype) { const int64_t size = dtype == TP_F32 ? 4 : 2; return Bytes{p, ld * size, cols * size}; }
 bool apart(const Bytes& a, const Bytes& b, int64_t rows) { return !a.p || !b.p || !rows_overlap(a.p, a.pitch, a.width, b.p, b.pitch, b.width, rows); }
 // An output and an input are one block, whose elements a thread reads before it writes them, or apart
-bool over_or_apart(const Bytes& out, const Bytes& in, int64_t rows) { return (out.p == in.p && out.pitch == in.pitch && out.width == in.width) || apart(out, in, rows); }
+bool over_or_apart(const Bytes& out, const Bytes& in, int64_t rows) {
+    return (out.p == in.p && out.width == in.width && (out.pitch == in.pitch || rows == 1)) || apart(out, in, rows);
+}
 
 // ---------------------------------------------------------------------------------------------
 // adapters
@@ -69,7 +71,7 @@ int check_factor(const void* ptr, int64_t ld, int64_t stride, const tp_adapters_
 }
 // an operand and the output over it: the same block or apart
 int check_over(const tp_oblk_t& c, const tp_oblk_t& y, int64_t rows, int64_t cols) {
-    if (c.ptr == y.ptr && c.ld == y.ld && c.dtype == y.dtype) return TP_OK;
+    if (c.ptr == y.ptr && c.dtype == y.dtype && (c.ld == y.ld || rows == 1)) return TP_OK;
     const int64_t size = c.dtype == TP_F32 ? 4 : 2, size_y = y.dtype == TP_F32 ? 4 : 2;
     return rows_overlap(c.ptr, c.ld * size, cols * size, y.ptr, y.ld * size_y, cols * size_y, rows) ? TP_ERR_SHAPE : TP_OK;
 }

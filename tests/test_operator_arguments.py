@@ -171,6 +171,8 @@ def test_dropout_outputs_that_overlap_what_is_read_are_refused():
     assert f((at, 128, bf), (at + 128, 128, bf), res=(at, 128)) == 2                                                                          # columns of one matrix
     assert f((at, cols, f32), (at, cols, bf)) == 4 and f((at, cols, bf), (at, cols, f32)) == 4 and f((at, cols, f32), (at, 2 * cols, bf)) == 4  # other types, other strides
     assert f((at, cols, bf), (at, 72, bf)) == 4 and f((at, cols, bf), (at + 16, cols, bf)) == 4 and f((at, cols, bf), (at - 128 * 31, cols, bf)) == 4 and f((at, cols, bf), (at + 128 * 31, cols, bf)) == 4
+    one = lambda y: status(lambda: T.tp_dropout_fwd(NO, (at, 64, bf), None, T.EPI_NONE, y, rows=1, cols=cols, stream=0))
+    assert one((at, 128, bf)) == 2 and one((at, 64, bf)) == 2 and one((at, 64, f32)) == 4 and one((at + 16, 64, bf)) == 4                       # one row: the same whatever the stride
     assert f((at, cols, bf), (at + 128 * 32, cols, bf)) == 2 and f((at, cols, bf), (at - 128 * 32, cols, bf)) == 2
     assert f((at, cols, f32), far, res=(0x900000, 72)) == 4 and f((at, cols, f32), (0x900000, cols, f32), res=(0x900000, cols)) == 4
     assert f((at, cols, f32), far, pre=far) == 4 and f((at, cols, f32), far, pre=(at, cols, bf)) == 4 and f((at, cols, f32), far, res=(0x500000, cols), pre=(0x500010, cols, bf)) == 4
