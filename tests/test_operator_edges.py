@@ -1,11 +1,10 @@
 """Dropout and adapters where values and blocks are unusual: blocks over and between one another, infinities beside padded ranks, values that bf16 cannot hold,
 adapters that no row uses, many segments."""
-import math
-
 import pytest
 import torch
 
 import paper_2110_14883_amd as T
+import test_adapter
 from test_adapter import BF, F32, _g, _strided
 from test_dropout import _mask, _rand, factor, near, slope64
 
@@ -179,3 +178,16 @@ def test_one_workspace_for_every_number_of_segments(m, pool, rank):
         for p, q in zip(both(count, room[:-64]), both(count, torch.empty(size(count), dtype=torch.uint8, device="cuda"))):
             assert torch.equal(p, q), count
     assert (room[-64:] == 0xFF).all()
+
+
+@pytest.mark.parametrize("rank,p", [(16, 0.0), (72, 0.3)])
+@pytest.mark.parametrize("single", [False, True])
+def test_over_a_thousand_segments(monkeypatch, rank, p, single):
+    """Ragged ones with empty ones between, and single rows: many rounds of 64 of a workgroup's walk over them, the same adapter again and again."""
+    def cuts(kind, m):
+        n = 1300
+        at = [min(m, i if single else i * m // n + i * 7 % 3) for i in range(n + 1)]
+        return sorted(at), [i * 5 % 7 - 1 if i % 3 else i // 400 for i in range(n)]
+
+    monkeypatch.setattr(test_adapter, "_cuts", cuts)
+    test_adapter.run_case(T.Grid(T.MODE_1D_COL), (1500, 72, 136), rank, None, p=p, seed=90)
