@@ -6,12 +6,12 @@
 //   down  [rows, K] x [rank, K]^T      both operands contraction-contiguous, through LDS
 //   up    [rows, rank] x [rank, cols]  the factor's 8 x 8 blocks transposed in registers
 //   grad  [rows, rank]^T x [rows, cols]  the same turn of the second operand, sums over rows
-// All three are bound by memory: the rank is at most 128, so a row of X or Y that is read takes 2 to 64 flops a byte.  V and U stay in fp32.  Where they
+// All three are bound by memory: with 8 to 128 ranks *down* and *grad* take 8 to 128 flops a byte of X or dY, *up* 2 to 64 a byte of C and its result.  V and U stay in fp32.  Where they
 // are a matrix operand they go in as a sum of bf16 terms, two (2^-17) for bf16 results and three (2^-25) for fp32 ones: the matrix
 // unit has the time, and rounding them once would cost a bf16 step of the adapters' part.
-// Measured (all of a call, us, and the bytes it cannot do without over that): one token of 4096 x 4096, 16 ranks 7.2; 96 tokens over 48 adapters 9.5; 5923
+// Measured (all of a call, us, and the bytes it cannot do without over that): one token of 4096 x 4096, 16 ranks 7.4; 96 tokens over 48 adapters 9.5; 5923
 // rows in 12 segments, 32 ranks, GeLU 56 (4.4 TB/s); 2048 x 4 x 2048 x 8192, 64 ranks, dropout 30 (3.5); backward of 16384 x 4096 x 4096, 16 ranks, dropout,
-// fp32 178 (4.5), of 32896 x 640 over 2 x 2560, 8 ranks 108 (4.3).  A large copy reaches 5.2 TB/s.
+// fp32 178 (4.5), of 32896 x 640 over 2 x 2560, 8 ranks, three quarters of the rows with an adapter 101 (3.6).  A large copy reaches 5.2 TB/s.
 //
 // Rows come in segments, a request each, described by device arrays.  A workgroup works on a tile of one segment's rows: it finds its tile from
 // the offsets itself (one trip to memory for up to 64 segments), so a call is the same launches whatever the lengths, and can be captured.  Offsets are
@@ -579,14 +579,15 @@ __global__ __launch_bounds__(384) void tp_adapter_up_kernel(const UpArgs p, cons
 constexpr int few_waves(int rb) { return rb <= 4 ? 8 : 4; }              // (as many as leave a wave its registers)
 template <int RB> struct FewShape {                                      // RB: blocks of 16 ranks
     static constexpr int WAVES = few_waves(RB), SLOT = (1 + RB) * 2048, FIT = 163840 / (WAVES * SLOT);
-    static constexpr int NS = RB == 1 ? 2 : FIT > 4 ? 4 : FIT;           // (up to 16 ranks two workgroups share a CU)
+    static constexpr int NS = RB == 1 ? 2 : FIT > 4 ? 4 : FIT;           // (up to 16 ranks, so that two workgroups share a CU where the registers allow it, below)
     static constexpr int PART = 16 * RB + 4, SUMS = WAVES * 16 * PART * 4;
     static constexpr int LOW = 16 * UpShape<2 * RB, 3>::ROW;             // behind the waves' sums, where the ring was
     static constexpr int BYTES = WAVES * NS * SLOT > SUMS + LOW ? WAVES * NS * SLOT : SUMS + LOW;
     static_assert(NS >= 1 && BYTES <= 163840);
 };
 // Up to 16 ranks and bf16 throughout the registers are held to what lets two workgroups share a CU (1000 single rows of 4096 x 4096 50 -> 35 us, one row 6.7 -> 6.5);
-// elsewhere that would spill (32 ranks, 1000 rows 57 -> 63).
+// elsewhere that would spill (32 ranks, 1000 rows 57 -> 63).  With an fp32 side up to 16 ranks take 134 to 152 registers: one workgroup a CU there, though the ring has
+// two slots for them too.
 constexpr int few_waves_a_simd(int rb, int terms, bool c32) { return rb == 1 && terms == 2 && !c32 ? 4 : 1; }
 template <int RB, int TERMS, bool C32>
 __global__ __launch_bounds__(64 * few_waves(RB), few_waves_a_simd(RB, TERMS, C32)) void tp_adapter_few_kernel(const DownArgs d, const UpArgs p) {
@@ -844,7 +845,8 @@ hipError_t up_as(const UpArgs& a, const GradArgs* fin, hipStream_t s) {
     const int waves = strip_waves > 1 ? strip_waves : a.tile * GP >= 256 ? 4 : (a.tile * GP + 63) / 64;
     UpArgs args = a;
     args.waves = strip_waves;
-    // (planes to add are there only where *grad* has under 512 workgroups: a few thousand more)
+    // (planes to add: of the whole pool, shares and pool 256 together at most or as many as make two workgroups of *grad* a CU; the places of adapters without rows
+    // add zeros.  128 workgroups for one adapter of 16384 x 4096 x 4096, 16 ranks; 131072 for a pool of 128 of 128 ranks)
     const int64_t more = fin ? ((int64_t)finish_blocks_each(*fin, 64 * waves) * fin->seg.pool * fin->sides + y - 1) / y : 0;
     const dim3 grid((unsigned)(a.tiles + more), (unsigned)y), block(64 * waves);
     const size_t lds = (size_t)a.tile * UpShape<GP, TERMS>::ROW;

@@ -132,9 +132,9 @@ bool in_one_launch(const Split& s, int64_t rows, int64_t segments, int64_t facto
     return factor <= (rows > 8 * segments ? most / 4 : most);
 }
 // Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 32 ranks each) of the adapters that can have rows for two a CU (four: 63 us
-// for 55, and more planes), but of four units of 32 rows (one a wave) at least, and at most two units on average; and room for 256 adapters' sums at most, where
-// that is more than the whole pool would ask for.  Backward in us, by rows and the whole pool before: 222 rows in 29 segments, 56 ranks 34.5 -> 24; 8814
-// rows, two of 12 adapters, 32 ranks 83.4 -> 67.9; 8124 rows in two segments, 27 adapters, 16 ranks 25.7 -> 22; without the average: 642 rows in 28
+// for 55, and more planes), but of four units of 32 rows (one a wave) at least where they are all one adapter's, and of two of an adapter's average; and room for
+// the planes of 256 adapters at most, or those that the whole pool would ask for (idle adapters have planes too, which nobody writes or reads).  Backward in
+// us, by rows and the whole pool before: 222 rows in 29 segments, 56 ranks 34.5 -> 24; 8814 rows, two of 12 adapters, 32 ranks 83.4 -> 67.9; 8124 rows in two segments, 27 adapters, 16 ranks 25.7 -> 22; without the average: 642 rows in 28
 // segments, ten adapters, 64 ranks 35 -> 21.
 int64_t grad_blocks(int64_t cols, int pool, int rank) { return (cols + 127) / 128 * ((rank + 31) / 32) * pool; }
 int64_t grad_busy(int64_t segments, int pool) { return std::max<int64_t>(1, std::min<int64_t>(pool, segments)); }     // adapters that can have rows
