@@ -330,7 +330,7 @@ typedef struct { uint64_t seed, offset; const uint64_t* offset_dev; int64_t row0
  *   x        : fp32 or bf16 (x_dtype) [rows, cols];  bias: bf16 [cols] or NULL with TP_EPI_NONE;
  *   residual : optional bf16 [rows, cols] (NULL ptr: none);  y: fp32 or bf16;  preact: optional bf16 copy of A.
  * y, or preact, may be x or residual itself (same address, type and leading dimension); apart from that neither may overlap these or the other
- * (TP_ERR_SHAPE; blocks whose rows lie equally far apart may lie between each other's rows, for others their spans count).  cols and every ld multiples of 8.  HBM-bound.
+ * (TP_ERR_SHAPE; rows equally far apart may lie between each other's, for others the spans count).  cols and every ld multiples of 8.  HBM-bound.
  * Defined by: Section 2.2, 1D paragraph and the chunk shapes of 2D / 2.5D / 3D, as tp_bias_act: what is applied to a rank's chunk of the output
  * once it exists.  Nothing is done with rows = 0 or cols = 0 (blocks may be NULL then).
  * Errors: TP_ERR_NULL, TP_ERR_MODE, TP_ERR_SHAPE, TP_ERR_ALIGN, TP_ERR_DTYPE, TP_ERR_HIP.
@@ -340,8 +340,10 @@ int tp_dropout_fwd(const tp_dropout_t* drop, const void* x, int64_t ld_x, int x_
 
 /*
  * tp_dropout_bwd -- its gradient:  dx = drop'(dy) GeLU'(preact)  (without preact: drop'(dy)), bf16, and optionally db (fp32 [cols]): the
- * column sums of dx before its rounding, in an order fixed by (rows, cols) and whether there is a workspace (up to 2^30 - 256 columns then, else TP_ERR_SHAPE).  The residual's gradient is dy itself.
- *   drop      : as in forward.   dy, preact, dx: bf16 [rows, cols];  dx may be dy or preact itself (same leading dimension), else must not overlap it (TP_ERR_SHAPE).
+ * column sums of dx before its rounding, in an order fixed by (rows, cols) and whether there is a workspace (up to 2^30 - 256 columns then, else
+ * TP_ERR_SHAPE).  The residual's gradient is dy itself.
+ *   drop      : as in forward.   dy, preact, dx: bf16 [rows, cols];  dx may be dy or preact itself (same leading dimension), else must not overlap
+ *               it (TP_ERR_SHAPE).
  *   workspace : as in tp_bias_grad (tp_bias_grad_workspace_size(rows, cols) bytes, 16-byte aligned, or NULL); read only if db is wanted.
  * With rows = 0 db is all zeros (blocks may be NULL then).  Errors: as tp_dropout_fwd, and TP_ERR_WORKSPACE.
  */
@@ -375,7 +377,8 @@ typedef struct { void* ptr; int64_t ld, stride; } tp_factor_out_t;
  *   drop     : dropout on the adapters' input, or NULL.  Positions are those in the full X [M, H] (the library adds the blocks' own), behind
  *              row0, col0.
  *   c, y     : [m, n], fp32 or bf16 each: the shared product (tp_linear_fwd with TP_EPI_NONE) and the output.  y may be c itself (same address, type and
- *              leading dimension), else the two must not overlap (TP_ERR_SHAPE; rows equally far apart may lie between each other's, else the spans count).   bias, epi, preact: as in tp_linear_fwd.
+ *              leading dimension), else the two must not overlap (TP_ERR_SHAPE; rows equally far apart may lie between each other's, for others the
+ *              spans count).   bias, epi, preact: as in tp_linear_fwd.
  *   v        : optional fp32 [m, rank], rows rank apart: V, saved for backward (rows without an adapter are not written).
  *   workspace: >= tp_adapter_workspace_size(.., TP_PASS_FWD, ..) bytes, 16-byte aligned; one call's at a time.
  * Apart from y over c no output may overlap an input or another output.

@@ -6,9 +6,9 @@
 //   down  [rows, K] x [rank, K]^T      both operands contraction-contiguous, through LDS
 //   up    [rows, rank] x [rank, cols]  the factor's 8 x 8 blocks transposed in registers
 //   grad  [rows, rank]^T x [rows, cols]  the same turn of the second operand, sums over rows
-// All three are bound by memory: with 8 to 128 ranks *down* and *grad* take 8 to 128 flops a byte of X or dY, *up* 2 to 64 a byte of C and its result.  V and U stay in fp32.  Where they
-// are a matrix operand they go in as a sum of bf16 terms, two (2^-17) for bf16 results and three (2^-25) for fp32 ones: the matrix
-// unit has the time, and rounding them once would cost a bf16 step of the adapters' part.
+// All three are bound by memory: with 8 to 128 ranks *down* and *grad* take 8 to 128 flops a byte of X or dY, *up* 2 to 64 a byte of C and its result.
+// V and U stay in fp32.  Where they are a matrix operand they go in as a sum of bf16 terms, two (2^-17) for bf16 results and three (2^-25) for fp32 ones:
+// the matrix unit has the time, and rounding them once would cost a bf16 step of the adapters' part.
 // Measured (all of a call, us, and the bytes it cannot do without over that): one token of 4096 x 4096, 16 ranks 7.4; 96 tokens over 48 adapters 9.5; 5923
 // rows in 12 segments, 32 ranks, GeLU 56 (4.4 TB/s); 2048 x 4 x 2048 x 8192, 64 ranks, dropout 30 (3.5); backward of 16384 x 4096 x 4096, 16 ranks, dropout,
 // fp32 178 (4.5), of 32896 x 640 over 2 x 2560, 8 ranks, three quarters of the rows with an adapter 101 (3.6).  A large copy reaches 5.2 TB/s.
@@ -586,8 +586,8 @@ template <int RB> struct FewShape {                                      // RB: 
     static_assert(NS >= 1 && BYTES <= 163840);
 };
 // Up to 16 ranks and bf16 throughout the registers are held to what lets two workgroups share a CU (1000 single rows of 4096 x 4096 50 -> 35 us, one row 6.7 -> 6.5);
-// elsewhere that would spill (32 ranks, 1000 rows 57 -> 63).  With an fp32 side up to 16 ranks take 134 to 152 registers: one workgroup a CU there, though the ring has
-// two slots for them too.
+// elsewhere that would spill (32 ranks, 1000 rows 57 -> 63).  With an fp32 side up to 16 ranks take 134 to 152 registers: one workgroup a CU there,
+// though the ring has two slots for them too.
 constexpr int few_waves_a_simd(int rb, int terms, bool c32) { return rb == 1 && terms == 2 && !c32 ? 4 : 1; }
 template <int RB, int TERMS, bool C32>
 __global__ __launch_bounds__(64 * few_waves(RB), few_waves_a_simd(RB, TERMS, C32)) void tp_adapter_few_kernel(const DownArgs d, const UpArgs p) {

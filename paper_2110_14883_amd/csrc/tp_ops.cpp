@@ -134,8 +134,8 @@ bool in_one_launch(const Split& s, int64_t rows, int64_t segments, int64_t facto
 // Shares of an adapter's rows: enough workgroups (a strip of 128 columns by 32 ranks each) of the adapters that can have rows for two a CU (four: 63 us
 // for 55, and more planes), but of four units of 32 rows (one a wave) at least where they are all one adapter's, and of two of an adapter's average; and room for
 // the planes of 256 adapters at most, or those that the whole pool would ask for (idle adapters have planes too, which nobody writes or reads).  Backward in
-// us, by rows and the whole pool before: 222 rows in 29 segments, 56 ranks 34.5 -> 24; 8814 rows, two of 12 adapters, 32 ranks 83.4 -> 67.9; 8124 rows in two segments, 27 adapters, 16 ranks 25.7 -> 22; without the average: 642 rows in 28
-// segments, ten adapters, 64 ranks 35 -> 21.
+// us, by rows and the whole pool before: 222 rows in 29 segments, 56 ranks 34.5 -> 24; 8814 rows, two of 12 adapters, 32 ranks 83.4 -> 67.9; 8124 rows in
+// two segments, 27 adapters, 16 ranks 25.7 -> 22; without the average: 642 rows in 28 segments, ten adapters, 64 ranks 35 -> 21.
 int64_t grad_blocks(int64_t cols, int pool, int rank) { return (cols + 127) / 128 * ((rank + 31) / 32) * pool; }
 int64_t grad_busy(int64_t segments, int pool) { return std::max<int64_t>(1, std::min<int64_t>(pool, segments)); }     // adapters that can have rows
 int64_t grad_enough(int64_t cols, int rank, int64_t adapters) { const int64_t blocks = grad_blocks(cols, 1, rank) * adapters; return (512 + blocks - 1) / blocks; }
@@ -144,8 +144,9 @@ int plan_grad(int64_t rows, int64_t segments, int64_t cols, int pool, int rank) 
     const int64_t busy = grad_busy(segments, pool), units = most_tiles(rows, segments, 32);
     return (int)std::max<int64_t>(1, std::min<int64_t>({grad_enough(cols, rank, busy), grad_room(cols, pool, rank), units / 4, std::max<int64_t>(1, units / (2 * busy)), 32}));
 }
-// The most of these that any number of segments up to this one takes: a program has one workspace for batches of more and fewer requests.  K is shared most with
-// one segment, which has the fewest tiles (64 rows make more than 128 of them where they are chosen, and K is not shared then); of the shares every bound where it is largest.
+// The most of these that any number of segments up to this one takes: a program has one workspace for batches of more and fewer requests.  K is shared most
+// with one segment, which has the fewest tiles (64 rows make more than 128 of them where they are chosen, and K is not shared then); of the shares every
+// bound where it is largest.
 int most_splits(int64_t rows, int64_t k, int n_steps, int64_t up_cols, int rank, bool bwd) { return plan_products(rows, 1, k, n_steps, up_cols, rank, bwd).splits; }
 int most_shares(int64_t rows, int64_t segments, int64_t cols, int pool, int rank) {
     const int64_t units = most_tiles(rows, segments, 32), busy = segments > pool ? pool : 1;
